@@ -59,6 +59,7 @@ struct sd_timer; /* see the measurement aids at the end */
 
 #define SD_BF16 0
 #define SD_FP8_E4M3 1
+#define SD_F32 2 /* norm weights only (sd_qk_norm) */
 
 typedef struct {
     int32_t batch;              /* B >= 0 (0: the call is a no-op) */
@@ -345,6 +346,158 @@ int paged_prefill_attention(const sd_shape *shape, const void *q, const int32_t 
                             const float *k_scales, const float *v_scales,
                             const int32_t *block_table, const int32_t *context_lens,
                             float scale, float *out, void *stream, struct sd_timer *timer);
+
+/*
+ * Norms of queries and keys with the position rotation.
+ *
+ * The projections of a layer leave rows of queries, keys and values; before
+ * they are attended, every head's query and key is divided by its root mean
+ * square, weighted, and rotated to its token's position.  With x one head's
+ * row of d elements, w the norm's weights and pos the token's position:
+ *     r = 1 / sqrt(mean(x^2) + eps),  z = x r w,  y = R(pos) z
+ * R turns the first rotary_dim elements in pairs by the angles whose cosines
+ * and sines row pos of the table holds:
+ *     (u, v) -> (u cos - v sin, v cos + u sin)
+ * All arithmetic is fp32; y is rounded to bf16 once.
+ *
+ *   q, k, v        bf16: token t's heads lie at q + t * q_stride (elements), one after the other;
+ *                  a fused projection's rows are taken as they are
+ *   q_weight, k_weight   [d], weight_dtype
+ *   rope_table     f32 [table_len][rotary_dim]: cosines of the pairs' angles, then their sines
+ *   positions      i32 [T]; outside [0, table_len) the nearest row of the table is taken.
+ *                  With rotary_dim == 0 neither is read (NULL)
+ */
+typedef struct {
+    int32_t num_q_heads, num_kv_heads;
+    int32_t head_dim;     /* 64 or 128 */
+    int32_t rotary_dim;   /* a multiple of 16, at most head_dim; 0: no rotation */
+    int32_t interleaved;  /* 0: pairs (i, i + rotary_dim / 2); 1: pairs (2 i, 2 i + 1) */
+    int32_t table_len;    /* rows of the table */
+    int32_t weight_dtype; /* SD_BF16 or SD_F32 */
+    float eps;            /* >= 0 */
+    int64_t q_stride;     /* elements between the rows of two tokens: at least the heads' elements, a */
+    int64_t k_stride;     /* multiple of 8; 0: rows lie side by side */
+    int64_t v_stride;     /* (of qk_norm_rope_append only) */
+} sd_qk_norm;
+
+/*
+ * qk_norm_rope -- rows to rows: a training step's forward pass, or the rows
+ * that kv_append_fp8 then quantises into an fp8 cache.
+ *
+ *   q_out, k_out   bf16 [T][heads][d]; may be q and k themselves where those lie side by side
+ * T == 0 is a no-op.
+ */
+int qk_norm_rope(const sd_qk_norm *norm, const void *q, const void *k, const void *q_weight, const void *k_weight,
+                 const float *rope_table, const int32_t *positions, int32_t T,
+                 void *q_out, void *k_out, void *stream);
+
+/*
+ * qk_norm_rope_append -- the same with the keys and the values written into
+ * their page slots, as kv_append does: row t belongs to sequence seq_ids[t]
+ * and goes to slot slots[t] of it; its rotation is that of positions[t].  The
+ * two differ where a cache has been cut down (kv_evict) and a token's place in
+ * it is no longer its position.
+ *
+ *   seq_ids   i32 [T] or NULL: row t belongs to sequence t
+ *   slots     i32 [T] or NULL: every token's slot is its position
+ *   q_out     bf16 [T][num_q_heads][d]
+ * A row whose sequence is outside [0, batch), whose slot is outside the block table or
+ * whose page is outside the pool is not stored (its q_out row is): a call of
+ * fixed size takes rows of sequence -1 for those it does not need.  Two rows
+ * that address the same slot race.  `norm` and `shape` must agree on heads and
+ * head_dim; no lengths enter, so shape->max_context_len is not looked at.  SD_BF16 pools only (SD_EUNSUPPORTED otherwise).
+ */
+int qk_norm_rope_append(const sd_shape *shape, const sd_qk_norm *norm, const void *q, const void *k, const void *v,
+                        const void *q_weight, const void *k_weight, const float *rope_table,
+                        const int32_t *positions, const int32_t *seq_ids, const int32_t *slots, int32_t T,
+                        void *q_out, void *k_pages, void *v_pages, const int32_t *block_table, void *stream);
+
+/*
+ * qk_norm_rope_backward -- the gradient of qk_norm_rope, from its inputs and
+ * the gradients dq_out, dk_out (bf16 [T][heads][d]) of its outputs:
+ *     dz = R^T dy,  dw = sum over rows of dz x r,  g = dz w,
+ *     dx = r (g - x r^2 mean(g x))
+ *
+ *   dq, dk               bf16, laid out as q and k (their strides); may be dq_out and dk_out where
+ *                        those strides leave no gap
+ *   dq_weight, dk_weight f32 [d], written; the rows are added in an order that
+ *                        depends on the sizes alone (results are reproducible bit for bit)
+ *   workspace            >= qk_norm_rope_workspace_bytes(norm, T) bytes, contents ignored
+ * T == 0 writes zeros to dq_weight and dk_weight.
+ */
+size_t qk_norm_rope_workspace_bytes(const sd_qk_norm *norm, int32_t T);
+int qk_norm_rope_backward(const sd_qk_norm *norm, const void *dq_out, const void *dk_out,
+                          const void *q, const void *k, const void *q_weight, const void *k_weight,
+                          const float *rope_table, const int32_t *positions, int32_t T,
+                          void *dq, void *dk, float *dq_weight, float *dk_weight,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * paged_weight_accumulate -- the attention weight that every cached token has
+ * received, brought up to date.
+ *
+ * A rollout whose cache is bounded keeps the tokens that later tokens look at.
+ * For each sequence b, KV head g and token t < L = min(context_lens[b], max_context_len):
+ *     scores_out[b][g][t] = decay * scores_in[b][g][t] + sum_rows softmax_t(scale * <q_row, K_t>)
+ * over the query rows of b and the query heads of g.  Without q_start there is
+ * one row per sequence, the query of its last token (a decode step).  With it
+ * sequence b owns the rows q_start[b] .. q_start[b+1]-1, as in
+ * paged_prefill_attention: row i of n_b is the query of position L - n_b + i
+ * and attends the tokens up to that one; rows of negative positions add
+ * nothing, nor do those past max_q_len (which should not exist: the bound is
+ * the caller's).  Weights and scores are fp32.
+ *
+ *   q            bf16 [total_q][num_q_heads][d]
+ *   q_start      i32 [batch + 1] or NULL (then total_q is batch and max_q_len 1); a sequence
+ *                whose range leaves [0, total_q) has no rows
+ *   k_scales     NULL for SD_BF16
+ *   new_tokens   the last new_tokens positions of every sequence count as 0 in scores_in,
+ *                whatever it holds there
+ *   scores_in    f32 [batch][num_kv_heads][score_stride], or NULL: zeros; may be scores_out
+ *   scores_out   f32, the same layout; entries at positions >= L are left as they are
+ *   score_stride at least max_context_len, a multiple of 4
+ *   workspace    >= paged_weight_workspace_bytes(shape, max_q_len) bytes, contents ignored
+ */
+size_t paged_weight_workspace_bytes(const sd_shape *shape, int32_t max_q_len);
+int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t *q_start,
+                            int32_t total_q, int32_t max_q_len,
+                            const void *k_pages, const float *k_scales,
+                            const int32_t *block_table, const int32_t *context_lens,
+                            float scale, float decay, int32_t new_tokens,
+                            const float *scores_in, float *scores_out, int64_t score_stride,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * kv_evict -- cuts the cache of every sequence down to `budget` tokens.
+ *
+ * Each (sequence, KV head) keeps its first `sinks` tokens, its last `recent`
+ * ones and, of those between, the ones with the largest scores (equal scores:
+ * the lower position; NaN counts as the lowest), budget in all; a sequence of at most
+ * `budget` tokens keeps all.  Heads keep different tokens, but as many: every
+ * sequence still has one length.  The rows that stay move, in their order,
+ * into the pages of new_block_table, so prefix pages that other trajectories
+ * share stay as they are; the old pages are the caller's to release.  Keys
+ * stay rotated to their own positions.
+ * fp8 pools: a new tile's scale is the largest of its rows' old scales; rows
+ * of a smaller one are re-encoded as code * (old / new), fp32, nearest e4m3fn.
+ *
+ *   sinks, recent      >= 0, sinks + recent <= budget
+ *   scores             f32 [batch][num_kv_heads][score_stride], score_stride >= max_context_len
+ *   block_table, new_block_table   i32 [batch][max_blocks_per_seq]; of the latter the first
+ *                      ceil(min(L, budget) / 16) entries are used.  A new page may be
+ *                      neither an old page of the call nor another sequence's new one
+ *   kept               i32 [batch][num_kv_heads][budget], written: the positions that stay, ascending, then -1
+ *   new_lens           i32 [batch], written: min(L, budget); may be context_lens
+ *   scores_out         f32 [batch][num_kv_heads][scores_out_stride] or NULL: the kept tokens'
+ *                      scores in their new places; stride >= min(budget, max_context_len);
+ *                      may be scores (equal strides)
+ */
+int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recent,
+             const float *scores, int64_t score_stride,
+             void *k_pages, void *v_pages, float *k_scales, float *v_scales,
+             const int32_t *block_table, const int32_t *context_lens,
+             const int32_t *new_block_table, int32_t *kept, int32_t *new_lens,
+             float *scores_out, int64_t scores_out_stride, void *stream);
 
 /*
  * Session prefix tree (host only; no device memory, no HIP calls).

@@ -7,7 +7,9 @@ fallback: if the shared library is missing, loading raises.
 """
 from .binding import (  # noqa: F401
     SD_BF16,
+    SD_F32,
     SD_FP8_E4M3,
+    QkNorm,
     SeamDecodeError,
     Shape,
     KernelTimer,
@@ -16,6 +18,7 @@ from .binding import (  # noqa: F401
     kv_append,
     kv_append_fp8,
     kv_copy_pages,
+    kv_evict,
     lib_path,
     load,
     paged_decode_attention,
@@ -23,7 +26,13 @@ from .binding import (  # noqa: F401
     paged_decode_attention_prefix,
     paged_decode_attention_static,
     paged_prefill_attention,
+    paged_weight_accumulate,
+    paged_weight_workspace_bytes,
     probe_read,
+    qk_norm_rope,
+    qk_norm_rope_append,
+    qk_norm_rope_backward,
+    qk_norm_rope_workspace_bytes,
     range_parts,
     strerror,
     validate_groups,

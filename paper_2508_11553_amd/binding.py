@@ -11,6 +11,7 @@ _lib = None
 
 SD_BF16 = 0
 SD_FP8_E4M3 = 1
+SD_F32 = 2
 
 
 class SeamDecodeError(RuntimeError):
@@ -32,6 +33,23 @@ class Shape(ctypes.Structure):
         ("kv_dtype", ctypes.c_int32),
         ("max_context_len", ctypes.c_int32),
         ("chunk_tokens", ctypes.c_int32),
+    ]
+
+
+class QkNorm(ctypes.Structure):
+    """Mirror of sd_qk_norm."""
+    _fields_ = [
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("table_len", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
     ]
 
 
@@ -82,6 +100,21 @@ def load():
     L.kv_copy_pages.argtypes = [sp, vp, vp, i32, vp, vp, vp, vp, vp]
     L.paged_prefill_attention.restype = ctypes.c_int
     L.paged_prefill_attention.argtypes = [sp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp]
+    np_, i64 = ctypes.POINTER(QkNorm), ctypes.c_int64
+    L.qk_norm_rope.restype = ctypes.c_int
+    L.qk_norm_rope.argtypes = [np_, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    L.qk_norm_rope_append.restype = ctypes.c_int
+    L.qk_norm_rope_append.argtypes = [sp, np_, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    L.qk_norm_rope_workspace_bytes.restype = sz
+    L.qk_norm_rope_workspace_bytes.argtypes = [np_, i32]
+    L.qk_norm_rope_backward.restype = ctypes.c_int
+    L.qk_norm_rope_backward.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.paged_weight_workspace_bytes.restype = sz
+    L.paged_weight_workspace_bytes.argtypes = [sp, i32]
+    L.paged_weight_accumulate.restype = ctypes.c_int
+    L.paged_weight_accumulate.argtypes = [sp, vp, vp, i32, i32, vp, vp, vp, vp, f32, f32, i32, vp, vp, i64, vp, sz, vp]
+    L.kv_evict.restype = ctypes.c_int
+    L.kv_evict.argtypes = [sp, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     L.sd_validate_tables.restype = ctypes.c_int
     L.sd_validate_tables.argtypes = [sp, vp, vp, vp, vp]
     L.sd_validate_groups.restype = ctypes.c_int
@@ -273,6 +306,58 @@ def paged_prefill_attention(shape: Shape, q, q_start, total_q: int, max_q_len: i
         _ptr(k_scales), _ptr(v_scales), _ptr(block_table), _ptr(context_lens), float(scale), _ptr(out),
         _stream(stream), timer._h if timer is not None else None)
     _check(rc, "paged_prefill_attention")
+
+
+def qk_norm_rope(norm: QkNorm, q, k, q_weight, k_weight, rope_table, positions, T: int, q_out, k_out, stream=None):
+    rc = load().qk_norm_rope(ctypes.byref(norm), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(rope_table),
+                             _ptr(positions), int(T), _ptr(q_out), _ptr(k_out), _stream(stream))
+    _check(rc, "qk_norm_rope")
+
+
+def qk_norm_rope_append(shape: Shape, norm: QkNorm, q, k, v, q_weight, k_weight, rope_table, positions, seq_ids, slots,
+                        T: int, q_out, k_pages, v_pages, block_table, stream=None):
+    rc = load().qk_norm_rope_append(ctypes.byref(shape), ctypes.byref(norm), _ptr(q), _ptr(k), _ptr(v), _ptr(q_weight),
+                                    _ptr(k_weight), _ptr(rope_table), _ptr(positions), _ptr(seq_ids), _ptr(slots),
+                                    int(T), _ptr(q_out), _ptr(k_pages), _ptr(v_pages), _ptr(block_table),
+                                    _stream(stream))
+    _check(rc, "qk_norm_rope_append")
+
+
+def qk_norm_rope_workspace_bytes(norm: QkNorm, T: int) -> int:
+    return int(load().qk_norm_rope_workspace_bytes(ctypes.byref(norm), int(T)))
+
+
+def qk_norm_rope_backward(norm: QkNorm, dq_out, dk_out, q, k, q_weight, k_weight, rope_table, positions, T: int, dq, dk,
+                          dq_weight, dk_weight, workspace, workspace_nbytes: int, stream=None):
+    rc = load().qk_norm_rope_backward(ctypes.byref(norm), _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(q_weight),
+                                      _ptr(k_weight), _ptr(rope_table), _ptr(positions), int(T), _ptr(dq), _ptr(dk),
+                                      _ptr(dq_weight), _ptr(dk_weight), _ptr(workspace), int(workspace_nbytes),
+                                      _stream(stream))
+    _check(rc, "qk_norm_rope_backward")
+
+
+def paged_weight_workspace_bytes(shape: Shape, max_q_len: int) -> int:
+    return int(load().paged_weight_workspace_bytes(ctypes.byref(shape), int(max_q_len)))
+
+
+def paged_weight_accumulate(shape: Shape, q, q_start, total_q: int, max_q_len: int, k_pages, k_scales, block_table,
+                            context_lens, scale: float, decay: float, new_tokens: int, scores_in, scores_out,
+                            score_stride: int, workspace, workspace_nbytes: int, stream=None):
+    rc = load().paged_weight_accumulate(ctypes.byref(shape), _ptr(q), _ptr(q_start), int(total_q), int(max_q_len),
+                                        _ptr(k_pages), _ptr(k_scales), _ptr(block_table), _ptr(context_lens),
+                                        float(scale), float(decay), int(new_tokens), _ptr(scores_in), _ptr(scores_out),
+                                        int(score_stride), _ptr(workspace), int(workspace_nbytes), _stream(stream))
+    _check(rc, "paged_weight_accumulate")
+
+
+def kv_evict(shape: Shape, budget: int, sinks: int, recent: int, scores, score_stride: int, k_pages, v_pages, k_scales,
+             v_scales, block_table, context_lens, new_block_table, kept, new_lens, scores_out=None,
+             scores_out_stride: int = 0, stream=None):
+    rc = load().kv_evict(ctypes.byref(shape), int(budget), int(sinks), int(recent), _ptr(scores), int(score_stride),
+                         _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(block_table),
+                         _ptr(context_lens), _ptr(new_block_table), _ptr(kept), _ptr(new_lens), _ptr(scores_out),
+                         int(scores_out_stride), _stream(stream))
+    _check(rc, "kv_evict")
 
 
 def validate_tables(shape: Shape, block_table, context_lens, report, stream=None):

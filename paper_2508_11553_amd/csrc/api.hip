@@ -693,6 +693,291 @@ int paged_prefill_attention(const sd_shape *shape, const void *q, const int32_t 
     return SD_OK;
 }
 
+}  // extern "C"
+
+namespace {
+
+// Stride of the rows of `heads` heads: 0 stands for rows side by side; no row may reach into the next, and rows start at 16 bytes.
+bool row_stride(int64_t stride, int heads, int head_dim, int64_t *out)
+{
+    const int64_t row = (int64_t)heads * head_dim;
+    *out = stride ? stride : row;
+    return stride == 0 || (stride >= row && stride % 8 == 0);
+}
+
+int check_norm(const sd_qk_norm *n)
+{
+    if (!n || n->num_q_heads <= 0 || n->num_kv_heads <= 0 || n->head_dim <= 0 || n->rotary_dim < 0 || n->rotary_dim > n->head_dim) return SD_EINVAL;
+    if (n->rotary_dim % 16 != 0 || (n->rotary_dim > 0 && n->table_len <= 0)) return SD_EINVAL;
+    if (n->interleaved != 0 && n->interleaved != 1) return SD_EINVAL;
+    if (n->weight_dtype != SD_BF16 && n->weight_dtype != SD_F32) return SD_EINVAL;
+    if (!(n->eps >= 0.f) || n->eps > 3e38f) return SD_EINVAL;
+    int64_t s;
+    if (!row_stride(n->q_stride, n->num_q_heads, n->head_dim, &s) || !row_stride(n->k_stride, n->num_kv_heads, n->head_dim, &s) ||
+        !row_stride(n->v_stride, n->num_kv_heads, n->head_dim, &s))
+        return SD_EINVAL;
+    if (n->head_dim != 64 && n->head_dim != 128) return SD_EUNSUPPORTED;
+    return SD_OK;
+}
+
+bool too_many_rows(const sd_qk_norm *n, int32_t T) { return (uint64_t)T * ((uint64_t)n->num_q_heads + 2 * (uint64_t)n->num_kv_heads) > sd::kMaxRows; }
+
+sd::NormRopeArgs norm_args(const sd_qk_norm *n, const void *q, const void *k, const void *q_weight, const void *k_weight, const float *rope_table,
+                           const int32_t *positions, int32_t T, void *q_out, void *k_out)
+{
+    sd::NormRopeArgs a;
+    a.q = static_cast<const uint16_t *>(q);
+    a.k = static_cast<const uint16_t *>(k);
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.table = rope_table;
+    a.positions = positions;
+    a.q_out = static_cast<uint16_t *>(q_out);
+    a.k_out = static_cast<uint16_t *>(k_out);
+    row_stride(n->q_stride, n->num_q_heads, n->head_dim, &a.q_stride);
+    row_stride(n->k_stride, n->num_kv_heads, n->head_dim, &a.k_stride);
+    a.T = T;
+    a.Hq = n->num_q_heads;
+    a.Hkv = n->num_kv_heads;
+    a.rotary_dim = n->rotary_dim;
+    a.table_len = n->table_len;
+    a.interleaved = n->interleaved;
+    a.fp32_weights = n->weight_dtype == SD_F32;
+    a.eps = n->eps;
+    return a;
+}
+
+bool bad_norm_pointers(const sd_qk_norm *n, const void *q, const void *k, const void *q_weight, const void *k_weight, const float *rope_table, const int32_t *positions)
+{
+    return bad_ptr(q) || bad_ptr(k) || bad_ptr(q_weight) || bad_ptr(k_weight) || (n->rotary_dim > 0 && (bad_ptr(rope_table) || bad_ptr(positions)));
+}
+
+// Workgroups of the gradient: the queries' rows and the keys' in proportion, about four workgroups to a compute unit of the largest device.
+void gradient_blocks(const sd_qk_norm *n, int32_t T, int *q_blocks, int *k_blocks)
+{
+    constexpr int64_t kWorkgroups = 2 * kMaxRangeWorkgroups;
+    const int64_t per = 256 / (n->head_dim / 16), heads = (int64_t)n->num_q_heads + n->num_kv_heads;   // rows a workgroup holds at a time
+    auto blocks = [&](int64_t h) { return (int)std::max<int64_t>(1, std::min((T * h + per - 1) / per, kWorkgroups * h / heads)); };
+    *q_blocks = blocks(n->num_q_heads);
+    *k_blocks = blocks(n->num_kv_heads);
+}
+
+// Sizes of paged_weight_accumulate.
+struct WeightPlan {
+    bool keep;                    // the products stay in the workspace between the steps
+    int64_t rows, pages, chunk_pages, chunks, apply_blocks;
+    size_t stats_off, rows_off, total;
+};
+WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
+{
+    WeightPlan w;
+    const int64_t units = (int64_t)s->batch * s->num_kv_heads;
+    w.rows = (int64_t)max_q_len * (s->num_q_heads / s->num_kv_heads);
+    w.keep = w.rows <= sd::kMaxGroup;
+    w.pages = std::max<int64_t>(1, ((int64_t)s->max_context_len + sd::kPage - 1) / sd::kPage);
+    w.chunk_pages = std::max<int64_t>(16, ((w.pages + 63) / 64 + 15) / 16 * 16);
+    w.chunks = (w.pages + w.chunk_pages - 1) / w.chunk_pages;
+    w.apply_blocks = (w.pages + 63) / 64;
+    const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    w.stats_off = w.keep ? up((size_t)units * w.pages * w.rows * sd::kPage * 4) : 0;
+    w.rows_off = w.stats_off + up((size_t)units * w.chunks * w.rows * 8);
+    w.total = w.rows_off + (w.keep ? 0 : up((size_t)units * w.rows * 8));
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qk_norm_rope(const sd_qk_norm *norm, const void *q, const void *k, const void *q_weight, const void *k_weight, const float *rope_table,
+                 const int32_t *positions, int32_t T, void *q_out, void *k_out, void *stream)
+{
+    const int rc = check_norm(norm);
+    if (rc) return rc;
+    if (T < 0) return SD_EINVAL;
+    if (T == 0) return SD_OK;
+    if (bad_norm_pointers(norm, q, k, q_weight, k_weight, rope_table, positions) || bad_ptr(q_out) || bad_ptr(k_out)) return SD_EINVAL;
+    if (too_many_rows(norm, T)) return SD_EUNSUPPORTED;
+    const hipError_t e = sd::launch_norm_rope(norm_args(norm, q, k, q_weight, k_weight, rope_table, positions, T, q_out, k_out), nullptr, norm->head_dim,
+                                              static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+int qk_norm_rope_append(const sd_shape *shape, const sd_qk_norm *norm, const void *q, const void *k, const void *v, const void *q_weight,
+                        const void *k_weight, const float *rope_table, const int32_t *positions, const int32_t *seq_ids, const int32_t *slots, int32_t T,
+                        void *q_out, void *k_pages, void *v_pages, const int32_t *block_table, void *stream)
+{
+    if (!shape) return SD_EINVAL;
+    sd_shape of_rows = *shape;
+    of_rows.max_context_len = of_rows.chunk_tokens = 0;   // no lengths enter
+    int rc = check_shape(&of_rows);
+    if (!rc) rc = check_norm(norm);
+    if (rc) return rc;
+    if (norm->num_q_heads != shape->num_q_heads || norm->num_kv_heads != shape->num_kv_heads || norm->head_dim != shape->head_dim) return SD_EINVAL;
+    if (T < 0) return SD_EINVAL;
+    if (shape->kv_dtype != SD_BF16) return SD_EUNSUPPORTED;
+    if (T == 0) return SD_OK;
+    if (bad_norm_pointers(norm, q, k, q_weight, k_weight, rope_table, positions) || bad_ptr(v) || bad_ptr(q_out) || bad_ptr(k_pages) || bad_ptr(v_pages) ||
+        bad_ptr(block_table) || (seq_ids && !aligned16(seq_ids)) || (slots && !aligned16(slots)) || (!slots && bad_ptr(positions)))
+        return SD_EINVAL;
+    if (too_many_rows(norm, T)) return SD_EUNSUPPORTED;
+    sd::RowPages p;
+    p.v = static_cast<const uint16_t *>(v);
+    row_stride(norm->v_stride, norm->num_kv_heads, norm->head_dim, &p.v_stride);
+    p.seq_ids = seq_ids;
+    p.slots = slots;
+    p.k_pages = static_cast<uint16_t *>(k_pages);
+    p.v_pages = static_cast<uint16_t *>(v_pages);
+    p.block_table = block_table;
+    p.batch = shape->batch;
+    p.max_blocks = shape->max_blocks_per_seq;
+    p.num_pages = shape->num_pages;
+    const hipError_t e = sd::launch_norm_rope(norm_args(norm, q, k, q_weight, k_weight, rope_table, positions, T, q_out, nullptr), &p, norm->head_dim,
+                                              static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+size_t qk_norm_rope_workspace_bytes(const sd_qk_norm *norm, int32_t T)
+{
+    if (check_norm(norm) || T < 0) return 0;
+    int q_blocks, k_blocks;
+    gradient_blocks(norm, T, &q_blocks, &k_blocks);
+    return (size_t)(q_blocks + k_blocks) * norm->head_dim * 4;
+}
+
+int qk_norm_rope_backward(const sd_qk_norm *norm, const void *dq_out, const void *dk_out, const void *q, const void *k, const void *q_weight,
+                          const void *k_weight, const float *rope_table, const int32_t *positions, int32_t T, void *dq, void *dk, float *dq_weight,
+                          float *dk_weight, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_norm(norm);
+    if (rc) return rc;
+    if (T < 0 || bad_ptr(dq_weight) || bad_ptr(dk_weight) || bad_ptr(workspace)) return SD_EINVAL;
+    if (T > 0 && (bad_norm_pointers(norm, q, k, q_weight, k_weight, rope_table, positions) || bad_ptr(dq_out) || bad_ptr(dk_out) || bad_ptr(dq) || bad_ptr(dk)))
+        return SD_EINVAL;
+    if (T == 0 && (bad_ptr(q_weight) || bad_ptr(k_weight))) return SD_EINVAL;
+    if (too_many_rows(norm, T)) return SD_EUNSUPPORTED;
+    if (workspace_bytes < qk_norm_rope_workspace_bytes(norm, T)) return SD_EWORKSPACE;
+    sd::NormGradArgs d;
+    int k_blocks;
+    gradient_blocks(norm, T, &d.q_blocks, &k_blocks);
+    d.dq_out = static_cast<const uint16_t *>(dq_out);
+    d.dk_out = static_cast<const uint16_t *>(dk_out);
+    d.dq = static_cast<uint16_t *>(dq);
+    d.dk = static_cast<uint16_t *>(dk);
+    d.dq_weight = dq_weight;
+    d.dk_weight = dk_weight;
+    d.parts = static_cast<float *>(workspace);
+    d.per_q = sd::division_by(norm->num_q_heads);
+    d.per_k = sd::division_by(norm->num_kv_heads);
+    const hipError_t e = sd::launch_norm_rope_backward(norm_args(norm, q, k, q_weight, k_weight, rope_table, positions, T, nullptr, nullptr), d, k_blocks,
+                                                       norm->head_dim, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+size_t paged_weight_workspace_bytes(const sd_shape *shape, int32_t max_q_len)
+{
+    if (check_shape(shape) || max_q_len < 0) return 0;
+    return std::max<size_t>(256, weight_plan(shape, max_q_len).total);
+}
+
+int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t *q_start, int32_t total_q, int32_t max_q_len, const void *k_pages,
+                            const float *k_scales, const int32_t *block_table, const int32_t *context_lens, float scale, float decay, int32_t new_tokens,
+                            const float *scores_in, float *scores_out, int64_t score_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_shape(shape);
+    if (rc) return rc;
+    if (total_q < 0 || max_q_len < 0 || new_tokens < 0 || score_stride < shape->max_context_len || score_stride % 4 != 0) return SD_EINVAL;
+    if (!(scale == scale) || !(decay == decay)) return SD_EINVAL;
+    if (!q_start && (total_q != shape->batch || max_q_len != 1)) return SD_EINVAL;
+    if (shape->batch == 0 || shape->max_context_len == 0) return SD_OK;
+    if (bad_ptr(k_pages) || bad_ptr(block_table) || bad_ptr(context_lens) || bad_ptr(scores_out) || bad_ptr(workspace) || (total_q > 0 && bad_ptr(q)) ||
+        (q_start && !aligned16(q_start)) || (scores_in && !aligned16(scores_in)))
+        return SD_EINVAL;
+    if (shape->kv_dtype == SD_FP8_E4M3 && bad_ptr(k_scales)) return SD_EINVAL;
+    max_q_len = std::min(max_q_len, total_q);
+    const WeightPlan w = weight_plan(shape, max_q_len);
+    if (w.rows > 0x7fffffff || (int64_t)shape->batch * shape->num_kv_heads * std::max(w.chunks, w.apply_blocks) > 0x7fffffff) return SD_EUNSUPPORTED;
+    if (workspace_bytes < w.total) return SD_EWORKSPACE;
+    char *ws = static_cast<char *>(workspace);
+    sd::WeightArgs a;
+    a.q = static_cast<const uint16_t *>(q);
+    a.q_start = q_start;
+    a.k_pages = k_pages;
+    a.k_scales = k_scales;
+    a.block_table = block_table;
+    a.context_lens = context_lens;
+    a.scores_in = scores_in;
+    a.scores_out = scores_out;
+    a.products = reinterpret_cast<float *>(ws);
+    a.stats = reinterpret_cast<float2 *>(ws + w.stats_off);
+    a.rows = reinterpret_cast<float2 *>(ws + w.rows_off);
+    a.score_stride = score_stride;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    a.decay = decay;
+    a.B = shape->batch;
+    a.Hq = shape->num_q_heads;
+    a.Hkv = shape->num_kv_heads;
+    a.G = shape->num_q_heads / shape->num_kv_heads;
+    a.max_blocks = shape->max_blocks_per_seq;
+    a.max_context_len = shape->max_context_len;
+    a.total_q = total_q;
+    a.max_q_len = max_q_len;
+    a.new_tokens = new_tokens;
+    a.max_rows = (int32_t)w.rows;
+    a.max_pages = (int32_t)w.pages;
+    a.chunks = (int32_t)w.chunks;
+    a.chunk_pages = (int32_t)w.chunk_pages;
+    a.apply_blocks = (int32_t)w.apply_blocks;
+    a.per_group = sd::division_by(a.G);
+    const hipError_t e = sd::launch_weights(a, w.keep, shape->head_dim, shape->kv_dtype, static_cast<hipStream_t>(stream));
+    if (e == hipErrorNotSupported) return SD_EUNSUPPORTED;
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recent, const float *scores, int64_t score_stride, void *k_pages, void *v_pages,
+             float *k_scales, float *v_scales, const int32_t *block_table, const int32_t *context_lens, const int32_t *new_block_table, int32_t *kept,
+             int32_t *new_lens, float *scores_out, int64_t scores_out_stride, void *stream)
+{
+    const int rc = check_shape(shape);
+    if (rc) return rc;
+    if (budget <= 0 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SD_EINVAL;
+    if (score_stride < shape->max_context_len) return SD_EINVAL;
+    const int32_t most = std::min(budget, shape->max_context_len);   // tokens that stay of a sequence
+    if (scores_out && (scores_out_stride < most || (scores_out == scores && scores_out_stride != score_stride))) return SD_EINVAL;
+    if (shape->batch == 0) return SD_OK;
+    if (bad_ptr(scores) || bad_ptr(k_pages) || bad_ptr(v_pages) || bad_ptr(block_table) || bad_ptr(context_lens) || bad_ptr(new_block_table) || bad_ptr(kept) ||
+        bad_ptr(new_lens) || (scores_out && !aligned16(scores_out)))
+        return SD_EINVAL;
+    const bool fp8 = shape->kv_dtype == SD_FP8_E4M3;
+    if (fp8 && (bad_ptr(k_scales) || bad_ptr(v_scales))) return SD_EINVAL;
+    sd::EvictArgs a;
+    a.scores = scores;
+    a.scores_out = scores_out;
+    a.k_pages = k_pages;
+    a.v_pages = v_pages;
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.block_table = block_table;
+    a.new_table = new_block_table;
+    a.context_lens = context_lens;
+    a.kept = kept;
+    a.new_lens = new_lens;
+    a.score_stride = score_stride;
+    a.scores_out_stride = scores_out_stride;
+    a.B = shape->batch;
+    a.Hkv = shape->num_kv_heads;
+    a.max_blocks = shape->max_blocks_per_seq;
+    a.max_context_len = shape->max_context_len;
+    a.budget = budget;
+    a.sinks = sinks;
+    a.recent = recent;
+    a.new_pages = std::max(1, (most + sd::kPage - 1) / sd::kPage);
+    if ((int64_t)a.B * a.Hkv * a.new_pages > 0x7fffffff) return SD_EUNSUPPORTED;
+    const hipError_t e = sd::launch_evict(a, shape->head_dim, shape->kv_dtype, static_cast<hipStream_t>(stream));
+    if (e == hipErrorNotSupported) return SD_EUNSUPPORTED;
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
 sd_timer *sd_timer_create(int32_t max_calls)
 {
     if (max_calls <= 0) return nullptr;

@@ -588,6 +588,88 @@ struct ValidateGroupsArgs {
     int32_t B, max_blocks, max_context_len, num_groups, max_group_size, max_shared_len;
 };
 
+// x / by for 0 <= x < 2^31 by a product: with 2^l >= by, m = floor(2^(31 + l) / by) + 1 is at most 2^32 - 1 for by > 1 and exceeds
+// 2^(31 + l) / by by e <= 1, so that the error x e / 2^(31 + l) stays below 1 / by.
+struct Division {
+    uint32_t m, shift;   // m == 0: by == 1
+    __host__ __device__ uint32_t of(uint32_t x) const { return m ? (uint32_t)((uint64_t)x * m >> 32) >> shift : x; }
+};
+__host__ inline Division division_by(uint32_t by)
+{
+    if (by <= 1) return Division{0, 0};
+    int l = 0;
+    while (((uint64_t)1 << l) < by) ++l;
+    return Division{(uint32_t)((((uint64_t)1 << (31 + l)) / by) + 1), (uint32_t)(l - 1)};
+}
+constexpr uint64_t kMaxRows = 0x7fffffff;   // head rows of one call: half a terabyte of them
+
+// Rows of the norm and rotation (norm_rope.hip): x rows of q and k at strides, y rows contiguous.
+struct NormRopeArgs {
+    const uint16_t *q, *k;               // bf16, token t's heads at t * stride
+    const void *q_weight, *k_weight;     // [d], bf16 or fp32
+    const float *table;                  // [table_len][rotary_dim]: cosines, then sines
+    const int32_t *positions;            // [T]
+    uint16_t *q_out, *k_out;             // [T][heads][d]
+    int64_t q_stride, k_stride;          // elements
+    int32_t T, Hq, Hkv, rotary_dim, table_len;
+    int32_t interleaved, fp32_weights;
+    float eps;
+};
+// Where the keys' and values' rows of the appending form go.
+struct RowPages {
+    const uint16_t *v;
+    int64_t v_stride;
+    const int32_t *seq_ids, *slots;      // [T]; null: row t is sequence t's, its slot is its position
+    uint16_t *k_pages, *v_pages;
+    const int32_t *block_table;
+    int32_t batch, max_blocks, num_pages;
+    Division per_token;                  // of a call's rows
+};
+struct NormGradArgs {
+    const uint16_t *dq_out, *dk_out;     // [T][heads][d]
+    uint16_t *dq, *dk;                   // laid out as q and k
+    float *dq_weight, *dk_weight;        // [d]
+    float *parts;                        // [workgroups][d]
+    int32_t q_blocks;                    // workgroups that walk the queries' rows
+    Division per_q, per_k;               // rows of a token
+};
+
+// Attention weights into running scores (weight_scores.hip).
+struct WeightArgs {
+    const uint16_t *q;                   // [total_q][Hq][d]
+    const int32_t *q_start;              // [B + 1]; null: row b is sequence b's
+    const void *k_pages;
+    const float *k_scales;
+    const int32_t *block_table, *context_lens;
+    const float *scores_in;              // [B][Hkv][score_stride]; null: zeros
+    float *scores_out;
+    float *products;                     // [B][Hkv][max_pages][max_rows][16]: a decode step's, log2 domain
+    float2 *stats;                       // [B][Hkv][chunks][max_rows]: (max, sum) of a chunk
+    float2 *rows;                        // [B][Hkv][max_rows]: (max, 1 / sum) of a row
+    int64_t score_stride;
+    float scale_log2e, decay;
+    int32_t B, Hq, Hkv, G, max_blocks, max_context_len, total_q, max_q_len, new_tokens;
+    int32_t max_rows;                    // query rows of a (sequence, KV head): max_q_len * G
+    int32_t max_pages;                   // of a sequence
+    int32_t chunks, chunk_pages;         // chunks of a sequence, pages of a chunk (a multiple of 16)
+    int32_t apply_blocks;                // workgroups of the second step per (sequence, KV head)
+    Division per_group;                  // by G
+};
+
+// Cutting a cache down (kv_evict.hip).
+struct EvictArgs {
+    const float *scores;                 // [B][Hkv][score_stride]
+    float *scores_out;                   // [B][Hkv][scores_out_stride] or null
+    void *k_pages, *v_pages;
+    float *k_scales, *v_scales;
+    const int32_t *block_table, *new_table, *context_lens;
+    int32_t *kept;                       // [B][Hkv][budget]
+    int32_t *new_lens;
+    int64_t score_stride, scores_out_stride;
+    int32_t B, Hkv, max_blocks, max_context_len, budget, sinks, recent;
+    int32_t new_pages;                   // of a sequence: ceil(min(budget, max_context_len) / 16)
+};
+
 // Launchers: enqueue on `stream`, return the hipError_t of the launch.  When
 // `start`/`stop` are given they are bound to the kernel's own begin and end
 // timestamps (hipExtLaunchKernelGGL), so their elapsed time is the kernel's
@@ -602,6 +684,10 @@ hipError_t launch_merge(const MergeArgs &a, int head_dim, hipStream_t stream,
                         hipEvent_t start = nullptr, hipEvent_t stop = nullptr);
 hipError_t launch_prefill(const PrefillArgs &a, int head_dim, int kv_dtype, hipStream_t stream,
                           hipEvent_t start = nullptr, hipEvent_t stop = nullptr);
+hipError_t launch_norm_rope(const NormRopeArgs &n, const RowPages *pages, int head_dim, hipStream_t stream);
+hipError_t launch_norm_rope_backward(const NormRopeArgs &n, const NormGradArgs &d, int k_blocks, int head_dim, hipStream_t stream);
+hipError_t launch_weights(const WeightArgs &a, bool keep, int head_dim, int kv_dtype, hipStream_t stream);
+hipError_t launch_evict(const EvictArgs &a, int head_dim, int kv_dtype, hipStream_t stream);
 hipError_t launch_append(const AppendArgs &a, int head_dim, hipStream_t stream);
 hipError_t launch_append_fp8(const AppendFp8Args &a, int head_dim, hipStream_t stream);
 hipError_t launch_copy_pages(const CopyPagesArgs &a, hipStream_t stream);
