@@ -764,24 +764,51 @@ void gradient_blocks(const sd_qk_norm *n, int32_t T, int *q_blocks, int *k_block
 
 // Sizes of paged_weight_accumulate.
 struct WeightPlan {
-    bool keep;                    // the products stay in the workspace between the steps
-    int64_t rows, pages, chunk_pages, chunks, apply_blocks;
+    int pack;                     // pages to a tile of products that the workspace keeps between the steps; 0: more rows than a tile has, none are kept
+    int whole_waves;              // waves of the one kernel that does both steps, else 0
+    int64_t rows, wave_tiles, blocks, block_tokens, tiles, apply_blocks, row_blocks;
     size_t stats_off, rows_off, total;
 };
 WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
 {
     WeightPlan w;
-    const int64_t units = (int64_t)s->batch * s->num_kv_heads;
-    w.rows = (int64_t)max_q_len * (s->num_q_heads / s->num_kv_heads);
-    w.keep = w.rows <= sd::kMaxGroup;
-    w.pages = std::max<int64_t>(1, ((int64_t)s->max_context_len + sd::kPage - 1) / sd::kPage);
-    w.chunk_pages = std::max<int64_t>(16, ((w.pages + 63) / 64 + 15) / 16 * 16);
-    w.chunks = (w.pages + w.chunk_pages - 1) / w.chunk_pages;
-    w.apply_blocks = (w.pages + 63) / 64;
+    const int64_t units = (int64_t)s->batch * s->num_kv_heads, tokens = std::max(1, s->max_context_len);
+    const auto parts = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
     const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-    w.stats_off = w.keep ? up((size_t)units * w.pages * w.rows * sd::kPage * 4) : 0;
-    w.rows_off = w.stats_off + up((size_t)units * w.chunks * w.rows * 8);
-    w.total = w.rows_off + (w.keep ? 0 : up((size_t)units * w.rows * 8));
+    w.rows = (int64_t)max_q_len * (s->num_q_heads / s->num_kv_heads);
+    w.pack = w.rows <= sd::kMaxGroup ? sd::weight_pack(w.rows) : 0;
+    const int64_t row_bytes = (int64_t)s->head_dim * (s->kv_dtype == SD_BF16 ? 2 : 1);
+    // One kernel, a workgroup per (sequence, KV head), while a workgroup's registers hold the products.  It saves a launch and the products' way
+    // through memory (32 of 288 bytes a token twice, 8 heads over a bf16 pool), but a lone workgroup reads at 46 GB/s: so either there are about as many
+    // of them as compute units, or the longest is short.  us, one kernel : two, lengths to the bound (8 heads a group; even lengths, bf16 unless said):
+    //   8 units      600 7.9 : 9.5   1200 11.2 : 9.5   fp8 1200 9.4 : 9.2      64 units   1200 11.9 : 12.2   4096 28 : 21   fp8 1200 10.0 : 11.2   4096 20.9 : 16.6
+    //   96 units    1200 12.3 : 13.5 4096 32 : 29      fp8 4096 22.8 : 21.7   128 units  1200 13.2 : 15.8   8192 60 : 66   mixed lengths 54 : 43
+    //   192 units   4096 38 : 50     8192 71 : 96      mixed 60 : 61           384 units  8192 155 : 176     mixed 108 : 112   fp8 8192 95 : 120
+    w.whole_waves = 0;
+    if (w.pack && (units >= 160 || tokens * row_bytes <= (128 + 3 * units) * 1024)) {
+        const int64_t per_wave = (int64_t)sd::whole_tiles(w.pack) * w.pack * sd::kPage;
+        w.whole_waves = units <= 256 ? 8 : 4;   // (600 tokens: 8 units 7.9 with 8 waves, 8.7 with 4; 384 units fp8 11.7 and 11.4)
+        while (w.whole_waves < 16 && w.whole_waves * per_wave < tokens) w.whole_waves *= 2;
+        if (w.whole_waves * per_wave < tokens) w.whole_waves = 0;
+    }
+    if (w.pack) {
+        // A wave's pages: two while that makes no more than 2500 waves, else four (32 units of 4096 14.7 : 13.9, 64 of 1200 12.2 : 12.6); and
+        // no more than 128 workgroups to a sequence, whose statistics every workgroup of the second step reads.
+        const int64_t pages = parts(tokens, sd::kPage);
+        w.wave_tiles = std::max<int64_t>(parts(units * pages > 5000 ? 4 : 2, w.pack), parts(pages, 128 * sd::kWaves * w.pack));
+    } else {
+        // Groups of four pages: as many workgroups as run at once, or a multiple (8 sequences of 5 k - 8 k, 8 KV heads, 256 rows: 16 groups 86, 8 97, 4 92).
+        const int64_t groups = units * parts(tokens, 4 * sd::kPage), slots = kMaxRangeWorkgroups;
+        w.wave_tiles = std::max<int64_t>(1, parts(groups, slots * parts(groups, slots * sd::kMaxGroups)));
+    }
+    w.block_tokens = sd::kPage * w.wave_tiles * (w.pack ? sd::kWaves * w.pack : 4);
+    w.blocks = parts(tokens, w.block_tokens);
+    w.tiles = w.pack ? parts(tokens, w.pack * sd::kPage) : 0;
+    w.apply_blocks = parts(tokens, 1024);
+    w.row_blocks = parts(w.rows, 64);
+    w.stats_off = up((size_t)units * w.tiles * 1024);
+    w.rows_off = w.stats_off + up((size_t)units * w.blocks * (w.pack ? sd::kMaxGroup / w.pack : w.rows) * 8);
+    w.total = w.rows_off + (w.pack ? 0 : up((size_t)units * w.rows * 8));
     return w;
 }
 
@@ -896,7 +923,7 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
     if (shape->kv_dtype == SD_FP8_E4M3 && bad_ptr(k_scales)) return SD_EINVAL;
     max_q_len = std::min(max_q_len, total_q);
     const WeightPlan w = weight_plan(shape, max_q_len);
-    if (w.rows > 0x7fffffff || (int64_t)shape->batch * shape->num_kv_heads * std::max(w.chunks, w.apply_blocks) > 0x7fffffff) return SD_EUNSUPPORTED;
+    if (w.rows > 0x7fffffff || (int64_t)shape->batch * shape->num_kv_heads * std::max({w.blocks, w.apply_blocks, w.row_blocks}) > 0x7fffffff) return SD_EUNSUPPORTED;
     if (workspace_bytes < w.total) return SD_EWORKSPACE;
     char *ws = static_cast<char *>(workspace);
     sd::WeightArgs a;
@@ -912,7 +939,8 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
     a.stats = reinterpret_cast<float2 *>(ws + w.stats_off);
     a.rows = reinterpret_cast<float2 *>(ws + w.rows_off);
     a.score_stride = score_stride;
-    a.scale_log2e = scale * 1.4426950408889634f;
+    a.scale_log2e = (scale < 0 ? -scale : scale) * 1.4426950408889634f;
+    a.q_flip = scale < 0 ? 0x80008000u : 0u;
     a.decay = decay;
     a.B = shape->batch;
     a.Hq = shape->num_q_heads;
@@ -924,12 +952,15 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
     a.max_q_len = max_q_len;
     a.new_tokens = new_tokens;
     a.max_rows = (int32_t)w.rows;
-    a.max_pages = (int32_t)w.pages;
-    a.chunks = (int32_t)w.chunks;
-    a.chunk_pages = (int32_t)w.chunk_pages;
+    a.max_tiles = (int32_t)w.tiles;
+    a.whole_waves = w.whole_waves;
+    a.wave_tiles = (int32_t)w.wave_tiles;
+    a.blocks = (int32_t)w.blocks;
+    a.block_tokens = (int32_t)w.block_tokens;
     a.apply_blocks = (int32_t)w.apply_blocks;
+    a.row_blocks = (int32_t)w.row_blocks;
     a.per_group = sd::division_by(a.G);
-    const hipError_t e = sd::launch_weights(a, w.keep, shape->head_dim, shape->kv_dtype, static_cast<hipStream_t>(stream));
+    const hipError_t e = sd::launch_weights(a, w.pack, shape->head_dim, shape->kv_dtype, static_cast<hipStream_t>(stream));
     if (e == hipErrorNotSupported) return SD_EUNSUPPORTED;
     return e == hipSuccess ? SD_OK : hip_fail(e);
 }

@@ -635,6 +635,10 @@ struct NormGradArgs {
 };
 
 // Attention weights into running scores (weight_scores.hip).
+constexpr int kMaxGroups = 16;    // groups of four pages that a workgroup walks where the products are made twice
+constexpr int whole_tiles(int pack) { return pack == 4 ? 8 : 16; }   // tiles of products that a wave's registers hold where both steps are one
+// Pages that share a tile of products, of at most 16 rows.
+constexpr int weight_pack(int64_t rows) { return rows <= 4 ? 4 : rows <= 8 ? 2 : 1; }
 struct WeightArgs {
     const uint16_t *q;                   // [total_q][Hq][d]
     const int32_t *q_start;              // [B + 1]; null: row b is sequence b's
@@ -643,16 +647,20 @@ struct WeightArgs {
     const int32_t *block_table, *context_lens;
     const float *scores_in;              // [B][Hkv][score_stride]; null: zeros
     float *scores_out;
-    float *products;                     // [B][Hkv][max_pages][max_rows][16]: a decode step's, log2 domain
-    float2 *stats;                       // [B][Hkv][chunks][max_rows]: (max, sum) of a chunk
+    float *products;                     // [B][Hkv][max_tiles][64 lanes][4]: a decode step's, log2 domain
+    float2 *stats;                       // (max, sum) of a row over a stretch of tokens.  Products kept: [B][Hkv][blocks][16 / pack], else [B][Hkv][blocks][max_rows]
     float2 *rows;                        // [B][Hkv][max_rows]: (max, 1 / sum) of a row
     int64_t score_stride;
-    float scale_log2e, decay;
+    float scale_log2e, decay;            // |scale| * log2(e)
+    uint32_t q_flip;                     // 0x80008000 when scale < 0: every query element changes sign as it is loaded
     int32_t B, Hq, Hkv, G, max_blocks, max_context_len, total_q, max_q_len, new_tokens;
     int32_t max_rows;                    // query rows of a (sequence, KV head): max_q_len * G
-    int32_t max_pages;                   // of a sequence
-    int32_t chunks, chunk_pages;         // chunks of a sequence, pages of a chunk (a multiple of 16)
-    int32_t apply_blocks;                // workgroups of the second step per (sequence, KV head)
+    int32_t max_tiles;                   // tiles of products of a sequence
+    int32_t whole_waves;                 // both steps in one: waves of a workgroup, else 0
+    int32_t wave_tiles;                  // products kept: tiles of a wave in the first step; else groups of four pages that a workgroup walks, at most kMaxGroups
+    int32_t blocks, block_tokens;        // workgroups of the first step per (sequence, KV head); tokens of one
+    int32_t apply_blocks;                // workgroups of the second step per (sequence, KV head), products kept
+    int32_t row_blocks;                  // workgroups that join the rows' statistics, products made again
     Division per_group;                  // by G
 };
 
@@ -686,7 +694,7 @@ hipError_t launch_prefill(const PrefillArgs &a, int head_dim, int kv_dtype, hipS
                           hipEvent_t start = nullptr, hipEvent_t stop = nullptr);
 hipError_t launch_norm_rope(const NormRopeArgs &n, const RowPages *pages, int head_dim, hipStream_t stream);
 hipError_t launch_norm_rope_backward(const NormRopeArgs &n, const NormGradArgs &d, int k_blocks, int head_dim, hipStream_t stream);
-hipError_t launch_weights(const WeightArgs &a, bool keep, int head_dim, int kv_dtype, hipStream_t stream);
+hipError_t launch_weights(const WeightArgs &a, int pack, int head_dim, int kv_dtype, hipStream_t stream);
 hipError_t launch_evict(const EvictArgs &a, int head_dim, int kv_dtype, hipStream_t stream);
 hipError_t launch_append(const AppendArgs &a, int head_dim, hipStream_t stream);
 hipError_t launch_append_fp8(const AppendFp8Args &a, int head_dim, hipStream_t stream);

@@ -2,26 +2,25 @@
 //
 //   s'[b][g][t] = decay s[b][g][t] + sum_rows softmax_t(scale <q_row, K_t>)      rows: the query rows of sequence b, heads of KV head g
 //
-// A weight needs its row's maximum and sum over all tokens, so there are two steps: one pass over K that makes the
-// products and leaves every chunk's (max, sum) for each row, and one over the tokens that turns products into weights.
+// A weight needs its row's maximum and sum over all tokens, so there are two steps: one over K that makes the products and
+// leaves (max, sum) of every stretch of tokens for each row, and one over the tokens that turns products into weights.
 // The products of one tile of 16 query rows (a decode step: the heads of a KV head) are kept in fp32 between the two,
-// rows * 4 bytes a token, a small part of K's 64 to 256; with more rows (the last tokens of a prompt) K is read again, from
-// the caches or memory, and multiplied again.
+// rows * 4 bytes a token, a small part of K's 64 to 256; with more rows (the last tokens of a prompt) K is read and multiplied again.
 //
 //   S[token][row] = K_page[token][d] . Q^T[d][row]     mfma 16x16x32 bf16, a page of 16 tokens at a time
 //
 // A lane holds four tokens (4 (lane / 16) ..) of row lane % 16.  K goes from memory straight into operand layout: lane n + 16 c
 // reads 16 bytes of token n; which d these are differs between pools, and Q is read in the same order.
 // Weights, sums and scores are fp32 throughout.
+#include <type_traits>
+
 #include "attn_tile.h"
 
 namespace sd {
 
 namespace {
 
-constexpr int kScorePages = 4;   // pages in a wave's registers at a time
-
-// One page of K as the first operand: lane n + 16 c holds token n.
+// One page of K: lane n + 16 c holds token n.  operand(s): the first operand of step s of the product.
 template <int D>
 struct Bf16Rows {
     static constexpr int kDim = D;
@@ -29,14 +28,8 @@ struct Bf16Rows {
     static constexpr bool kScaled = false;
     u32x4 k[D / 32];
     SD_DEV static int q_offset(int s, int c) { return 32 * s + 8 * c; }
-    template <bool STREAM>
-    SD_DEV void load(const char *page, int lane)
-    {
-        const char *p = page + (lane & 15) * (D * 2) + (lane >> 4) * 16;
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) k[s] = kv_load<STREAM>(reinterpret_cast<const u32x4 *>(p + s * 64));
-    }
     SD_DEV u32x4 operand(int s) const { return k[s]; }
+    static constexpr int kRowBytes = 2 * D;
 };
 template <int D>
 struct Fp8Rows {
@@ -45,19 +38,52 @@ struct Fp8Rows {
     static constexpr bool kScaled = true;
     u32x4 k[D / 64];   // 16 codes each
     SD_DEV static int q_offset(int s, int c) { return 64 * (s / 2) + 16 * c + 8 * (s % 2); }
-    template <bool STREAM>
-    SD_DEV void load(const char *page, int lane)
-    {
-        const char *p = page + (lane & 15) * D + (lane >> 4) * 16;
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) k[j] = kv_load<STREAM>(reinterpret_cast<const u32x4 *>(p + j * 64));
-    }
     SD_DEV u32x4 operand(int s) const
     {
         const unsigned lo = k[s / 2][2 * (s % 2)], hi = k[s / 2][2 * (s % 2) + 1];
         return u32x4{cvt_pk_bf16_fp8<false>(lo), cvt_pk_bf16_fp8<true>(lo), cvt_pk_bf16_fp8<false>(hi), cvt_pk_bf16_fp8<true>(hi)};
     }
+    static constexpr int kRowBytes = D;
 };
+
+// A page on its way through LDS.  Lanes in operand layout ask for 64 bytes of each of 16 rows at a time, half a cache line; a workgroup that
+// has a compute unit to itself gets 26 GB/s that way and 46 with loads of whole rows.  So 64 lanes bring 1 KB in one piece straight into
+// LDS, 16 bytes each: piece p of row r goes to place p ^ (r mod the row's pieces), by which source a lane asks for, so that
+// 16 rows' pieces of one column lie in different banks.
+template <class K>
+struct Staged {
+    static constexpr int kNt = 2;   // cache policy bit nt
+    static constexpr int kPieces = K::kRowBytes / 16, kLoads = K::kBytes / 1024;
+    SD_DEV static void issue(const char *page, char *slot, int lane)
+    {
+#pragma unroll
+        for (int s = 0; s < kLoads; ++s) {
+            const int at = 64 * s + lane, r = at / kPieces, p = at % kPieces ^ r % kPieces;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(page + r * K::kRowBytes + p * 16),
+                                             (__attribute__((address_space(3))) void *)(slot + s * 1024), 16, 0, kNt);
+        }
+    }
+    SD_DEV static void fetch(K &k, const char *slot, int lane)
+    {
+        const int r = lane & 15, c = lane >> 4;
+#pragma unroll
+        for (int s = 0; s < kLoads; ++s) k.k[s] = *reinterpret_cast<const u32x4 *>(slot + r * K::kRowBytes + ((4 * s + c) ^ r % kPieces) * 16);
+    }
+};
+// Waits for all but the newest N loads of this wave; for its LDS reads.  (s_waitcnt: vmcnt in bits 0-3 and 14-15, expcnt 4-6, lgkmcnt 8-11.)
+template <int N>
+SD_DEV void wait_loads()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+    asm volatile("" ::: "memory");
+}
+SD_DEV void wait_reads()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
+}
 
 // What a workgroup knows of its sequence.
 struct Sequence {
@@ -78,7 +104,7 @@ SD_DEV Sequence sequence_of(const WeightArgs &a, int b)
     return s;
 }
 
-// Row r of (sequence, KV head): query r / G, head r % G of the group.
+// Row r of (sequence, KV head): query r / G, head r % G of the group.  The scale's sign is the queries' (q_flip): scaling keeps the order.
 template <class K>
 SD_DEV void load_q(u32x4 (&q)[K::kDim / 32], const WeightArgs &a, const Sequence &s, int g, int r, int rows, int lane)
 {
@@ -86,35 +112,14 @@ SD_DEV void load_q(u32x4 (&q)[K::kDim / 32], const WeightArgs &a, const Sequence
     const uint16_t *p = a.q + ((int64_t)(s.first_q + i) * a.Hq + g * a.G + (r - i * a.G)) * K::kDim;
 #pragma unroll
     for (int j = 0; j < K::kDim / 32; ++j)
-        q[j] = r < rows ? *reinterpret_cast<const u32x4 *>(p + K::q_offset(j, lane >> 4)) : u32x4{0, 0, 0, 0};
+        q[j] = r < rows ? *reinterpret_cast<const u32x4 *>(p + K::q_offset(j, lane >> 4)) ^ a.q_flip : u32x4{0, 0, 0, 0};
 }
 
 // The tokens that row r attends: those before `end`.
 SD_DEV int row_end(const WeightArgs &a, const Sequence &s, int r, int rows) { return r < rows ? min(s.L, s.L - s.n + 1 + (int)a.per_group.of(r)) : 0; }
 
-template <class K>
-SD_DEV f32x4 products(const K &k, const u32x4 (&q)[K::kDim / 32], float scale)
-{
-    f32x4 x = {0, 0, 0, 0};
-#pragma unroll
-    for (int s = 0; s < K::kDim / 32; ++s) x = mfma_bf16_k32(k.operand(s), q[s], x);
-    return x * scale;
-}
-
-// The pages of tiles [first, first + kScorePages) of a sequence; pages past the last one repeat it (their tokens are masked).
-template <class K, bool STREAM>
-SD_DEV void load_pages(K (&k)[kScorePages], float (&scale)[kScorePages], const WeightArgs &a, ConstTable bt, int g, int first, int last, int lane)
-{
-#pragma unroll
-    for (int i = 0; i < kScorePages; ++i) {
-        const int64_t at = (int64_t)bt[min(first + i, last)] * a.Hkv + g;
-        k[i].template load<STREAM>(static_cast<const char *>(a.k_pages) + at * K::kBytes, lane);
-        scale[i] = K::kScaled ? ((ConstScales)a.k_scales)[at] * a.scale_log2e : a.scale_log2e;
-    }
-}
-
 struct Stat {
-    float m, l;   // running maximum (log2 domain) and sum of exp2(x - m)
+    float m, l;   // maximum (log2 domain) and sum of exp2(x - m)
 };
 SD_DEV float shrink_of(float from, float to) { return from == to ? 1.f : __builtin_amdgcn_exp2f(from - to); }   // (both may be -inf)
 SD_DEV Stat joined(Stat x, Stat y)
@@ -122,207 +127,539 @@ SD_DEV Stat joined(Stat x, Stat y)
     const float m = fmaxf(x.m, y.m);
     return Stat{m, x.l * shrink_of(x.m, m) + y.l * shrink_of(y.m, m)};
 }
-SD_DEV Stat over_lanes(Stat s, int from, int to)
-{
-    for (int off = from; off < to; off *= 2) s = joined(s, Stat{__shfl_xor(s.m, off, 64), __shfl_xor(s.l, off, 64)});
-    return s;
-}
-
-// x of four tokens (t0 ..), those before `end` attended: into the lane's statistics.
-SD_DEV void take(Stat &s, const f32x4 (&x)[kScorePages], int t0, int end)
-{
-    float m = s.m;
-#pragma unroll
-    for (int i = 0; i < kScorePages; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m = t0 + 16 * i + e < end ? fmaxf(m, x[i][e]) : m;
-    s.l *= shrink_of(s.m, m);
-    s.m = m;
-#pragma unroll
-    for (int i = 0; i < kScorePages; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s.l += t0 + 16 * i + e < end ? __builtin_amdgcn_exp2f(x[i][e] - m) : 0.f;
-}
 
 }  // namespace
 
-// First step: workgroup (sequence, chunk, KV head), KV head fastest; its waves take the chunk's pages in turn, kScorePages at a time.
-// KEEP: one tile of rows, whose products are kept.
-template <class K, bool KEEP>
-__global__ __launch_bounds__(kWaves * 64) void weight_stats_kernel(WeightArgs a)
+// A tile of few rows takes PACK pages: with W = 16 / PACK at least the rows, the rows stand W columns apart PACK times, every page's
+// product gives all of them, and column n keeps that of page n / W.  So every lane holds four tokens of a row (row n % W), the
+// exponentials are as many as there are products, and a tile of them is 1 KB in one piece.
+template <int PACK>
+struct Packed {
+    static constexpr int kRows = kMaxGroup / PACK;
+    int row, page, quarter;   // of the lane: row, page of the tile, four tokens of the page
+    SD_DEV explicit Packed(int lane) : row(lane & (kRows - 1)), page((lane & 15) / kRows), quarter(lane >> 4) {}
+    SD_DEV int token() const { return kPage * page + 4 * quarter; }   // the lane's first, counted from the tile's first
+};
+
+// A wave's walk over pages of one (sequence, KV head): those whose ids lanes 0 .. pages - 1 hold.  Two are on their way or in the wave's two
+// slots of LDS: while it works on one, the next comes.
+template <class K>
+struct Walk {
+    const char *pool;   // + id * stride: the page's tile of this head
+    int64_t stride;
+    char *slots;
+    int ids, pages, lane;
+    float scales;
+    SD_DEV Walk(const WeightArgs &a, int b, int g, int page, int count, char *lds, int lane_) : slots(lds), pages(count), lane(lane_)
+    {   // `page`: the lane's; `count`: of the wave
+        ids = a.block_table[(int64_t)b * a.max_blocks + page];
+        scales = K::kScaled ? a.k_scales[(int64_t)ids * a.Hkv + g] * a.scale_log2e : a.scale_log2e;
+        stride = (int64_t)a.Hkv * K::kBytes;
+        pool = static_cast<const char *>(a.k_pages) + (int64_t)g * K::kBytes;
+    }
+    SD_DEV void issue(int i) const
+    {
+        if (i < pages) Staged<K>::issue(pool + __builtin_amdgcn_readlane(ids, i) * stride, slots + i % 2 * K::kBytes, lane);
+    }
+    SD_DEV void start() const
+    {
+        wait_loads<0>();   // (what page() counts are its own loads)
+        issue(0);
+        issue(1);
+    }
+    // Scaled products of page i, which comes after i - 1.
+    SD_DEV f32x4 page(int i, const u32x4 (&q)[K::kDim / 32]) const
+    {
+        if (i + 1 < pages) wait_loads<Staged<K>::kLoads>();
+        else wait_loads<0>();
+        K k;
+        Staged<K>::fetch(k, slots + i % 2 * K::kBytes, lane);
+        wait_reads();
+        issue(i + 2);
+        f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < K::kDim / 32; ++c) y = mfma_bf16_k32(k.operand(c), q[c], y);
+        return y * (K::kScaled ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scales), i)) : scales);
+    }
+    // Of the PACK pages of tile i.
+    template <int PACK>
+    SD_DEV f32x4 tile(int i, const u32x4 (&q)[K::kDim / 32], const Packed<PACK> &at) const
+    {
+        f32x4 x = page(i * PACK, q);
+#pragma unroll
+        for (int j = 1; j < PACK; ++j) {
+            const f32x4 y = page(i * PACK + j, q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = at.page == j ? y[e] : x[e];
+        }
+        return x;
+    }
+};
+
+// First step of a decode step: a.wave_tiles tiles to a wave, KV head fastest in the grid.
+template <class K, int PACK>
+__global__ __launch_bounds__(kWaves * 64) void weight_products_kernel(WeightArgs a)
 {
-    __shared__ Stat s_stat[kWaves][kMaxGroup];
+    constexpr int W = kMaxGroup / PACK;
+    __shared__ __attribute__((aligned(16))) char s_pages[kWaves][2 * K::kBytes];
+    __shared__ Stat s_stat[kWaves][W];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int g = blockIdx.x % a.Hkv, c = blockIdx.x / a.Hkv % a.chunks, b = blockIdx.x / a.Hkv / a.chunks;
+    const int g = blockIdx.x % a.Hkv, c = blockIdx.x / a.Hkv % a.blocks, b = blockIdx.x / a.Hkv / a.blocks;
     const Sequence s = sequence_of(a, b);
-    const int rows = s.n * a.G, page0 = c * a.chunk_pages, last = (s.L + kPage - 1) / kPage - 1;
-    if (page0 > last || rows == 0) return;   // workgroup-uniform
-    const int page1 = min(last + 1, page0 + a.chunk_pages), n = lane & 15;
-    const ConstTable bt = (ConstTable)(a.block_table + (int64_t)b * a.max_blocks);
+    const int rows = s.n * a.G, last = (s.L + kPage - 1) / kPage - 1, all_tiles = last / PACK + 1, block0 = c * kWaves * a.wave_tiles;
+    if (block0 >= all_tiles || s.L == 0 || rows == 0) return;   // workgroup-uniform
     const int64_t unit = (int64_t)b * a.Hkv + g;
-    for (int r0 = 0; r0 < rows; r0 += kMaxGroup) {   // (one round with KEEP)
-        u32x4 q[K::kDim / 32];
-        load_q<K>(q, a, s, g, r0 + n, rows, lane);
-        const int end = row_end(a, s, r0 + n, rows);
-        Stat stat = {-INFINITY, 0.f};
-        for (int p = page0 + wave * kScorePages; p < page1; p += kWaves * kScorePages) {
-            K k[kScorePages];
-            float scale[kScorePages];
-            load_pages<K, KEEP>(k, scale, a, bt, g, p, last, lane);
-            f32x4 x[kScorePages];
+    const int tile0 = block0 + wave * a.wave_tiles, tiles = max(0, min(a.wave_tiles, all_tiles - tile0));
+    const Packed<PACK> at(lane);
+    const Walk<K> walk(a, b, g, min(tile0 * PACK + lane, last), tiles * PACK, s_pages[wave], lane);
+    u32x4 q[K::kDim / 32];
+    load_q<K>(q, a, s, g, at.row, rows, lane);
+    const int end = row_end(a, s, at.row, rows);
+    float *to = a.products + ((unit * a.max_tiles + tile0) * 64 + lane) * 4;
+    Stat stat = {-INFINITY, 0.f};
+    walk.start();
+    for (int i = 0; i < tiles; ++i) {
+        const f32x4 x = walk.tile(i, q, at);
+        *reinterpret_cast<f32x4 *>(to + i * 256) = x;
+        const int t0 = (tile0 + i) * PACK * kPage + at.token();
+        float m = stat.m;
 #pragma unroll
-            for (int i = 0; i < kScorePages; ++i) x[i] = products(k[i], q, scale[i]);
-            take(stat, x, p * kPage + 4 * (lane >> 4), end);
-            if (KEEP && n < rows) {   // [page][row][token]
-                float *to = a.products + ((unit * a.max_pages + p) * a.max_rows + n) * kPage + 4 * (lane >> 4);
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, t0 + e < end ? x[e] : -INFINITY);
+        float l = stat.l * shrink_of(stat.m, m);
 #pragma unroll
-                for (int i = 0; i < kScorePages; ++i)
-                    if (p + i < page1) *reinterpret_cast<f32x4 *>(to + (int64_t)i * a.max_rows * kPage) = x[i];
-            }
+        for (int e = 0; e < 4; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[e] - m);
+            l += t0 + e < end ? p : 0.f;
         }
-        stat = over_lanes(stat, 16, 64);
-        if (lane < 16) s_stat[wave][n] = stat;
-        __syncthreads();
-        if (threadIdx.x < 16 && r0 + n < rows) {
-            Stat all = s_stat[0][n];
+        stat = Stat{m, l};
+    }
+    for (int off = W; off < 64; off *= 2) stat = joined(stat, Stat{__shfl_xor(stat.m, off, 64), __shfl_xor(stat.l, off, 64)});
+    if (lane < W) s_stat[wave][lane] = stat;
+    __syncthreads();
+    if (threadIdx.x < W) {
+        Stat all = s_stat[0][lane];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) all = joined(all, s_stat[w][n]);
-            a.stats[(unit * a.chunks + c) * a.max_rows + r0 + n] = float2{all.m, all.l};
-        }
-        __syncthreads();
+        for (int w = 1; w < kWaves; ++w) all = joined(all, s_stat[w][lane]);
+        a.stats[(unit * a.blocks + c) * W + lane] = float2{all.m, all.l};
     }
 }
 
-// The statistics of a row over the sequence's chunks -> (max, 1 / sum), by one wave.
-SD_DEV float2 whole_row(const WeightArgs &a, int64_t unit, int r, int chunks, int lane)
+// x plus that of the lane's partners in the 2^k columns of a row's packed stretch (DPP adds).
+template <int W>
+SD_DEV float over_rows(float x)
 {
-    Stat s = {-INFINITY, 0.f};
-    for (int c = lane; c < chunks; c += 64) {
-        const float2 v = a.stats[(unit * a.chunks + c) * a.max_rows + r];
-        s = joined(s, Stat{v.x, v.y});
-    }
-    s = over_lanes(s, 1, 64);
-    return float2{s.m, 1.f / s.l};
+#define SD_DPP_ADD(ctrl) x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, 0xf, 0xf, false))
+    SD_DPP_ADD(0xb1);                  // quad_perm 1 0 3 2
+    SD_DPP_ADD(0x4e);                  // quad_perm 2 3 0 1
+    if (W >= 8) SD_DPP_ADD(0x141);     // row_half_mirror
+    if (W >= 16) SD_DPP_ADD(0x140);    // row_mirror
+#undef SD_DPP_ADD
+    return x;
 }
 
-// Second step after KEEP: four tokens to a thread, 1024 to a workgroup.
+// Its second step: kApplyTokens tokens to a workgroup, a tile at a time to a wave.
+constexpr int kApplyTokens = 1024;
+template <int PACK>
 __global__ __launch_bounds__(256) void weight_apply_kept_kernel(WeightArgs a)
 {
+    constexpr int W = kMaxGroup / PACK, T = kApplyTokens / kPage / PACK / 4;   // tiles of a wave
     __shared__ float2 s_row[kMaxGroup];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = blockIdx.x % a.Hkv, j = blockIdx.x / a.Hkv % a.apply_blocks, b = blockIdx.x / a.Hkv / a.apply_blocks;
     const Sequence s = sequence_of(a, b);
-    if (j * 1024 >= s.L) return;
+    if (j * kApplyTokens >= s.L) return;
     const int64_t unit = (int64_t)b * a.Hkv + g;
-    const int rows = s.n * a.G, chunks = (s.L + a.chunk_pages * kPage - 1) / (a.chunk_pages * kPage);
-    for (int r = wave; r < rows; r += 4) {
-        const float2 v = whole_row(a, unit, r, chunks, lane);
-        if (lane == 0) s_row[r] = v;
+    const int rows = s.n * a.G, tile0 = (j * 4 + wave) * T, tiles = (s.L + PACK * kPage - 1) / (PACK * kPage);
+    const Packed<PACK> at(lane);
+    // the products and the old scores are on their way while the statistics are joined
+    f32x4 x[T];
+    float before[T];
+    const int64_t scores = unit * a.score_stride;
+    const int t0 = tile0 * PACK * kPage + at.token(), mine = t0 + at.row;   // lane's first token; the one that it stores
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        if (tile0 + i < tiles && rows) x[i] = *reinterpret_cast<const f32x4 *>(a.products + ((unit * a.max_tiles + tile0 + i) * 64 + lane) * 4);
+        const int t = mine + i * PACK * kPage;
+        before[i] = a.scores_in && at.row < 4 && t < s.L - a.new_tokens ? a.scores_in[scores + t] : 0.f;
+    }
+    {   // row tid / 16, every 16th block to a lane
+        const int r = threadIdx.x / 16, from = threadIdx.x % 16, blocks = (s.L + a.block_tokens - 1) / a.block_tokens;
+        Stat sum = {-INFINITY, 0.f};
+        if (r < rows)
+            for (int c = from; c < blocks; c += 16) {
+                const float2 v = a.stats[(unit * a.blocks + c) * W + r];
+                sum = joined(sum, Stat{v.x, v.y});
+            }
+        for (int off = 1; off < 16; off *= 2) sum = joined(sum, Stat{__shfl_xor(sum.m, off, 64), __shfl_xor(sum.l, off, 64)});
+        if (from == 0) s_row[r] = float2{sum.m, 1.f / sum.l};
     }
     __syncthreads();
-    const int t0 = j * 1024 + threadIdx.x * 4;
-    if (t0 >= s.L) return;
-    const float *x = a.products + ((unit * a.max_pages + t0 / kPage) * a.max_rows) * kPage + t0 % kPage;
-    f32x4 sum = {0, 0, 0, 0};
-    for (int r = 0; r < rows; ++r) {
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(x + r * kPage);
-        const float2 row = s_row[r];
-        const int end = row_end(a, s, r, rows);
+    const float2 row = s_row[at.row];
+    const int end = row_end(a, s, at.row, rows);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += t0 + e < end ? __builtin_amdgcn_exp2f(v[e] - row.x) * row.y : 0.f;
+    for (int i = 0; i < T; ++i) {
+        if (tile0 + i < tiles) {   // wave-uniform
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[i][e] - row.x) * row.y;
+            const float all = over_rows<W>(t0 + i * PACK * kPage + e < end ? p : 0.f);
+            sum = at.row == e ? all : sum;
+        }
+        const int t = mine + i * PACK * kPage;
+        if (at.row < 4 && t < s.L) a.scores_out[scores + t] = sum + a.decay * before[i];
+        }
     }
-    const int64_t at = unit * a.score_stride + t0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (t0 + e < s.L) a.scores_out[at + e] = sum[e] + (a.scores_in && t0 + e < s.L - a.new_tokens ? a.decay * a.scores_in[at + e] : 0.f);
 }
 
-// Between the steps otherwise: every row's statistics once.
+// Both steps in one: a workgroup takes a whole (sequence, KV head) and its products stay in its registers, whole_tiles to a wave.
+template <class K, int PACK>
+__global__ __launch_bounds__(1024) void weight_whole_kernel(WeightArgs a)
+{
+    constexpr int T = whole_tiles(PACK), W = kMaxGroup / PACK;
+    extern __shared__ __attribute__((aligned(16))) char s_pages[];   // [waves][2][K::kBytes]
+    __shared__ Stat s_stat[16][W];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
+    const int g = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
+    const Sequence s = sequence_of(a, b);
+    if (s.L == 0) return;
+    const int64_t unit = (int64_t)b * a.Hkv + g;
+    const int rows = s.n * a.G, last = (s.L + kPage - 1) / kPage - 1, tiles = last / PACK + 1;
+    const Packed<PACK> at(lane);
+    // the wave's tile i is the sequence's tile i * waves + wave
+    const Walk<K> walk(a, b, g, min((lane / PACK * waves + wave) * PACK + lane % PACK, last), (wave < tiles ? (tiles - 1 - wave) / waves + 1 : 0) * PACK,
+                       s_pages + wave * (2 * K::kBytes), lane);
+    u32x4 q[K::kDim / 32];
+    load_q<K>(q, a, s, g, at.row, rows, lane);
+    const int end = row_end(a, s, at.row, rows);
+    const int64_t scores = unit * a.score_stride;
+    f32x4 x[T];
+    float m = -INFINITY;
+    walk.start();
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        const int tile = i * waves + wave;
+        if (tile >= tiles) break;   // wave-uniform
+        x[i] = walk.tile(i, q, at);
+        const int t0 = tile * PACK * kPage + at.token();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, t0 + e < end ? x[i][e] : -INFINITY);
+    }
+    for (int off = W; off < 64; off *= 2) m = fmaxf(m, __shfl_xor(m, off, 64));
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        const int tile = i * waves + wave;
+        if (tile >= tiles) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[i][e] = __builtin_amdgcn_exp2f(x[i][e] - m);
+            if (tile * PACK * kPage + at.token() + e >= end) x[i][e] = 0.f;
+            l += x[i][e];
+        }
+    }
+    for (int off = W; off < 64; off *= 2) l += __shfl_xor(l, off, 64);
+    float before[T];
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        const int t = (i * waves + wave) * PACK * kPage + at.token() + at.row;
+        before[i] = a.scores_in && at.row < 4 && t < s.L - a.new_tokens ? a.scores_in[scores + t] : 0.f;
+    }
+    if (lane < W) s_stat[wave][lane] = Stat{m, l};
+    __syncthreads();
+    Stat all = s_stat[0][at.row];
+    for (int w = 1; w < waves; ++w) all = joined(all, s_stat[w][at.row]);
+    const float weight = shrink_of(m, all.m) / all.l;
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        const int tile = i * waves + wave;
+        if (tile >= tiles) break;
+        const int t0 = tile * PACK * kPage + at.token(), t = t0 + at.row;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float v = over_rows<W>(t0 + e < end ? x[i][e] * weight : 0.f);
+            sum = at.row == e ? v : sum;
+        }
+        if (at.row < 4 && t < s.L) a.scores_out[scores + t] = sum + a.decay * before[i];
+    }
+}
+
+// More rows than a tile: they stay, kRowTiles tiles of them in each wave's registers, and K streams past.  A workgroup walks a.wave_tiles groups of
+// kGroupPages pages of one (sequence, KV head), once for every kRowTiles * 16 * waves rows; its waves bring a group into LDS, a page
+// each, and all read it as operands, kAtOnce pages at a time, while the next one comes.
+constexpr int kGroupPages = 4, kGroupTokens = kGroupPages * kPage, kAtOnce = 2;
+constexpr int kRowTiles = 2, kRowsOfWave = kRowTiles * kMaxGroup, kRowWaves = 8;
+template <class K>
+struct Stream {
+    static constexpr int S = K::kDim / 32;
+    const char *pool;   // + id * stride: the page's tile of this head
+    int64_t stride;
+    char *lds;          // [2][kGroupPages][K::kBytes]
+    int ids, lane, wave, waves, groups;   // ids: of the workgroup's pages, a lane each
+    float scales;
+    SD_DEV Stream(const WeightArgs &a, int b, int g, int page0, int last, int groups_, char *lds_, int lane_, int wave_, int waves_)
+        : lds(lds_), lane(lane_), wave(wave_), waves(waves_), groups(groups_)
+    {
+        ids = a.block_table[(int64_t)b * a.max_blocks + min(page0 + lane, last)];
+        scales = K::kScaled ? a.k_scales[(int64_t)ids * a.Hkv + g] * a.scale_log2e : a.scale_log2e;
+        stride = (int64_t)a.Hkv * K::kBytes;
+        pool = static_cast<const char *>(a.k_pages) + (int64_t)g * K::kBytes;
+    }
+    SD_DEV char *slot(int group, int i) const { return lds + ((group & 1) * kGroupPages + i) * K::kBytes; }
+    SD_DEV void issue(int group) const
+    {
+        for (int i = wave; i < kGroupPages; i += waves) Staged<K>::issue(pool + __builtin_amdgcn_readlane(ids, group * kGroupPages + i) * stride, slot(group, i), lane);
+    }
+    // Waits for a group, and sends the next one on its way: its slots were last read before the barrier.
+    SD_DEV void next(int group) const
+    {
+        wait_loads<0>();
+        __syncthreads();
+        if (group + 1 < groups) issue(group + 1);
+    }
+    // Operands of kAtOnce of its pages.
+    SD_DEV void fetch(int group, int first, u32x4 (&k)[kAtOnce][S], float (&scale)[kAtOnce]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            K page;
+            Staged<K>::fetch(page, slot(group, first + i), lane);
+#pragma unroll
+            for (int s = 0; s < S; ++s) k[i][s] = page.operand(s);
+            scale[i] = K::kScaled ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scales), group * kGroupPages + first + i)) : scales;
+        }
+    }
+};
+template <int STEPS>
+SD_DEV f32x4 products(const u32x4 (&k)[STEPS], const u32x4 (&q)[STEPS])
+{
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) x = mfma_bf16_k32(k[s], q[s], x);
+    return x;
+}
+
+// First step: every row's statistics over the workgroup's tokens.
+template <class K>
+__global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightArgs a)
+{
+    constexpr int S = K::kDim / 32;
+    __shared__ __attribute__((aligned(16))) char s_pages[2 * kGroupPages * K::kBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
+    const int g = blockIdx.x % a.Hkv, c = blockIdx.x / a.Hkv % a.blocks, b = blockIdx.x / a.Hkv / a.blocks;
+    const Sequence s = sequence_of(a, b);
+    const int rows = s.n * a.G, page0 = c * a.wave_tiles * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
+    if (page0 > last || rows == 0) return;   // workgroup-uniform (L == 0: last is -1)
+    const Stream<K> stream(a, b, g, page0, last, min(a.wave_tiles, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
+    float2 *stats = a.stats + (((int64_t)b * a.Hkv + g) * a.blocks + c) * a.max_rows;
+    for (int r0 = 0; r0 < rows; r0 += waves * kRowsOfWave) {
+        const int first = r0 + wave * kRowsOfWave;   // the wave's first row
+        if (r0) __syncthreads();   // the last group's readers
+        stream.issue(0);
+        u32x4 q[kRowTiles][S];
+        Stat stat[kRowTiles];
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i) {
+            load_q<K>(q[i], a, s, g, first + i * kMaxGroup + n, rows, lane);
+            stat[i] = Stat{-INFINITY, 0.f};
+        }
+        for (int group = 0; group < stream.groups; ++group) {
+            stream.next(group);
+            const int t0 = (page0 + group * kGroupPages) * kPage;
+            auto tiles = [&](auto masked) {
+#pragma unroll
+                for (int half = 0; half < kGroupPages; half += kAtOnce) {
+                    u32x4 k[kAtOnce][S];
+                    float scale[kAtOnce];
+                    stream.fetch(group, half, k, scale);
+#pragma unroll
+                    for (int i = 0; i < kRowTiles; ++i) {
+                        const int end = masked ? row_end(a, s, first + i * kMaxGroup + n, rows) - t0 - half * kPage - 4 * (lane >> 4) : 0;
+                        f32x4 x[kAtOnce];
+                        float m = stat[i].m, by[kAtOnce];   // by: what is left to multiply with
+#pragma unroll
+                        for (int p = 0; p < kAtOnce; ++p) {
+                            x[p] = products(k[p], q[i]);
+                            by[p] = masked ? 1.f : scale[p];
+                            if (masked)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) x[p][e] = 16 * p + e < end ? x[p][e] * scale[p] : -INFINITY;
+                            m = max_of(m, by[p] * max_of(max_of(x[p][0], x[p][1]), x[p][2], x[p][3]));
+                        }
+                        float l = stat[i].l * shrink_of(stat[i].m, m);
+#pragma unroll
+                        for (int p = 0; p < kAtOnce; ++p)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], by[p], -m));
+                                l += !masked || 16 * p + e < end ? w : 0.f;
+                            }
+                        stat[i] = Stat{m, l};
+                    }
+                }
+            };
+            if (first >= rows) continue;   // wave-uniform: rows that are not there
+            if (t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});   // every row attends all of these tokens
+            else tiles(std::true_type{});
+        }
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i) {
+            Stat all = stat[i];
+            for (int off = 16; off < 64; off *= 2) all = joined(all, Stat{__shfl_xor(all.m, off, 64), __shfl_xor(all.l, off, 64)});
+            const int r = first + i * kMaxGroup + n;
+            if (lane < 16 && r < rows) stats[r] = float2{all.m, all.l};
+        }
+    }
+}
+
+// Between the steps: every row's statistics over the sequence, four lanes to a row.
 __global__ __launch_bounds__(256) void weight_rows_kernel(WeightArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t unit = blockIdx.x;
+    const int64_t unit = blockIdx.x / a.row_blocks;
+    const int r = blockIdx.x % a.row_blocks * 64 + threadIdx.x % 64, slice = threadIdx.x / 64;
+    __shared__ Stat s_stat[4][64];
     const Sequence s = sequence_of(a, (int)(unit / a.Hkv));
-    const int chunks = (s.L + a.chunk_pages * kPage - 1) / (a.chunk_pages * kPage);
-    for (int r = threadIdx.x >> 6; r < s.n * a.G; r += 4) {
-        const float2 v = whole_row(a, unit, r, chunks, lane);
-        if (lane == 0) a.rows[unit * a.max_rows + r] = v;
+    const bool there = r < s.n * a.G;
+    const int blocks = (s.L + a.block_tokens - 1) / a.block_tokens;
+    Stat sum = {-INFINITY, 0.f};
+    if (there) {
+        const float2 *v = a.stats + unit * a.blocks * a.max_rows + r;
+        for (int c = slice; c < blocks; c += 32) {
+            float2 w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = v[(int64_t)min(c + 4 * i, blocks - 1) * a.max_rows];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + 4 * i < blocks) sum = joined(sum, Stat{w[i].x, w[i].y});
+        }
+    }
+    s_stat[slice][threadIdx.x % 64] = sum;
+    __syncthreads();
+    if (slice == 0 && there) {
+#pragma unroll
+        for (int i = 1; i < 4; ++i) sum = joined(sum, s_stat[i][threadIdx.x]);
+        a.rows[unit * a.max_rows + r] = float2{sum.m, 1.f / sum.l};
     }
 }
 
-// Second step with the products made again: grid as the first step's.
+// Second step: the products once more, and the weights' sums over the rows; grid as in the first.
 template <class K>
-__global__ __launch_bounds__(kWaves * 64) void weight_apply_kernel(WeightArgs a)
+__global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightArgs a)
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int g = blockIdx.x % a.Hkv, c = blockIdx.x / a.Hkv % a.chunks, b = blockIdx.x / a.Hkv / a.chunks;
+    constexpr int S = K::kDim / 32;
+    __shared__ __attribute__((aligned(16))) char s_pages[2 * kGroupPages * K::kBytes];
+    extern __shared__ float s_sum[];   // [waves][a.block_tokens]: a wave's sums over its rows
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
+    const int g = blockIdx.x % a.Hkv, c = blockIdx.x / a.Hkv % a.blocks, b = blockIdx.x / a.Hkv / a.blocks;
     const Sequence s = sequence_of(a, b);
-    const int rows = s.n * a.G, page0 = c * a.chunk_pages, last = (s.L + kPage - 1) / kPage - 1;
-    if (page0 > last) return;
-    const int page1 = min(last + 1, page0 + a.chunk_pages), n = lane & 15;
-    const ConstTable bt = (ConstTable)(a.block_table + (int64_t)b * a.max_blocks);
+    const int rows = s.n * a.G, page0 = c * a.wave_tiles * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
+    if (page0 > last) return;   // workgroup-uniform
     const int64_t unit = (int64_t)b * a.Hkv + g;
-    for (int p = page0 + wave * kScorePages; p < page1; p += kWaves * kScorePages) {
-        K k[kScorePages];
-        float scale[kScorePages];
-        load_pages<K, false>(k, scale, a, bt, g, p, last, lane);
-        f32x4 sum[kScorePages];
+    const Stream<K> stream(a, b, g, page0, last, min(a.wave_tiles, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
+    for (int r0 = 0; r0 < rows; r0 += waves * kRowsOfWave) {
+        const int first = r0 + wave * kRowsOfWave;
+        if (r0) __syncthreads();   // the last group's readers
+        stream.issue(0);
+        u32x4 q[kRowTiles][S];
+        float2 row[kRowTiles];
 #pragma unroll
-        for (int i = 0; i < kScorePages; ++i) sum[i] = f32x4{0, 0, 0, 0};
-        const int t0 = p * kPage + 4 * (lane >> 4);
-        for (int r0 = 0; r0 < rows; r0 += kMaxGroup) {
-            u32x4 q[K::kDim / 32];
-            load_q<K>(q, a, s, g, r0 + n, rows, lane);
-            const int end = row_end(a, s, r0 + n, rows);
-            const float2 row = a.rows[unit * a.max_rows + min(r0 + n, rows - 1)];
+        for (int i = 0; i < kRowTiles; ++i) {
+            const int r = first + i * kMaxGroup + n;
+            load_q<K>(q[i], a, s, g, r, rows, lane);
+            row[i] = r < rows ? a.rows[unit * a.max_rows + r] : float2{0.f, 0.f};
+        }
+        for (int group = 0; group < stream.groups; ++group) {
+            stream.next(group);
+            const int t0 = (page0 + group * kGroupPages) * kPage;
+            float mine = 0.f;   // over the tiles' rows: the 16 lanes of a group hold the same tokens; lane n keeps token n % 4 of page n / 4
+            auto tiles = [&](auto masked) {
 #pragma unroll
-            for (int i = 0; i < kScorePages; ++i) {
-                const f32x4 x = products(k[i], q, scale[i]);
+                for (int half = 0; half < kGroupPages; half += kAtOnce) {
+                    u32x4 k[kAtOnce][S];
+                    float scale[kAtOnce];
+                    stream.fetch(group, half, k, scale);
+                    f32x4 sum[kAtOnce];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[i][e] += t0 + 16 * i + e < end ? __builtin_amdgcn_exp2f(x[e] - row.x) * row.y : 0.f;
+                    for (int i = 0; i < kRowTiles; ++i) {
+                        const int end = masked ? row_end(a, s, first + i * kMaxGroup + n, rows) - t0 - half * kPage - 4 * (lane >> 4) : 0;
+#pragma unroll
+                        for (int p = 0; p < kAtOnce; ++p) {
+                            const f32x4 x = products(k[p], q[i]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale[p], -row[i].x));
+                                const float v = __builtin_fmaf(w, row[i].y, i ? sum[p][e] : 0.f);
+                                sum[p][e] = !masked || 16 * p + e < end ? v : i ? sum[p][e] : 0.f;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int p = 0; p < kAtOnce; ++p)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float v = over_rows<16>(sum[p][e]);
+                            mine = n == 4 * (half + p) + e ? v : mine;
+                        }
+                }
+            };
+            if (first < rows) {   // wave-uniform
+                // every row is there and attends all of these tokens (one that is not there gives 0 * K, which an infinite K makes NaN)
+                if (first + kRowsOfWave <= rows && t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});
+                else tiles(std::true_type{});
             }
+            float &kept = s_sum[wave * a.block_tokens + group * kGroupTokens + 16 * (n / 4) + 4 * (lane >> 4) + n % 4];
+            kept = r0 ? kept + mine : mine;
         }
-        // over the rows of the tile: the 16 lanes of a group hold the same tokens
-#pragma unroll
-        for (int i = 0; i < kScorePages; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                for (int off = 1; off < 16; off *= 2) sum[i][e] += __shfl_xor(sum[i][e], off, 64);
-        // lane n of a group stores token n % 4 of page n / 4
-        const int t = t0 + 16 * (n / 4) + n % 4;
-        float mine = 0.f;
-#pragma unroll
-        for (int i = 0; i < kScorePages; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mine = n == 4 * i + e ? sum[i][e] : mine;
-        if (t < min(s.L, page1 * kPage)) {
-            const int64_t at = unit * a.score_stride + t;
-            a.scores_out[at] = mine + (a.scores_in && t < s.L - a.new_tokens ? a.decay * a.scores_in[at] : 0.f);
-        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < stream.groups * kGroupTokens; i += blockDim.x) {
+        const int t = page0 * kPage + i;
+        if (t >= s.L) break;
+        float all = 0.f;
+        if (rows)
+            for (int w = 0; w < waves; ++w) all += s_sum[w * a.block_tokens + i];
+        const int64_t at = unit * a.score_stride + t;
+        a.scores_out[at] = all + (a.scores_in && t < s.L - a.new_tokens ? a.decay * a.scores_in[at] : 0.f);
     }
 }
 
 template <class K>
-static hipError_t launch_weights_of(const WeightArgs &a, bool keep, hipStream_t stream)
+static void launch_streamed(const WeightArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((int64_t)a.B * a.chunks * a.Hkv)), block(kWaves * 64);
-    if (keep) {
-        hipLaunchKernelGGL((weight_stats_kernel<K, true>), grid, block, 0, stream, a);
-        hipLaunchKernelGGL(weight_apply_kept_kernel, dim3((unsigned)((int64_t)a.B * a.apply_blocks * a.Hkv)), dim3(256), 0, stream, a);
-    } else {
-        hipLaunchKernelGGL((weight_stats_kernel<K, false>), grid, block, 0, stream, a);
-        hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)(a.B * a.Hkv)), dim3(256), 0, stream, a);
-        hipLaunchKernelGGL(weight_apply_kernel<K>, grid, block, 0, stream, a);
+    const dim3 grid((unsigned)((int64_t)a.B * a.blocks * a.Hkv)), block(std::max(1, std::min(kRowWaves, (a.max_rows + kRowsOfWave - 1) / kRowsOfWave)) * 64);
+    hipLaunchKernelGGL(weight_stats_kernel<K>, grid, block, 0, stream, a);
+    if (a.row_blocks) hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)((int64_t)a.B * a.Hkv * a.row_blocks)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(weight_apply_kernel<K>, grid, block, block.x / 64 * a.block_tokens * 4, stream, a);
+}
+
+template <class K, int PACK>
+static void launch_kept(const WeightArgs &a, hipStream_t stream)
+{
+    if (a.whole_waves) {
+        hipLaunchKernelGGL((weight_whole_kernel<K, PACK>), dim3((unsigned)((int64_t)a.B * a.Hkv)), dim3(a.whole_waves * 64), a.whole_waves * 2 * K::kBytes, stream, a);
+        return;
     }
+    hipLaunchKernelGGL((weight_products_kernel<K, PACK>), dim3((unsigned)((int64_t)a.B * a.blocks * a.Hkv)), dim3(kWaves * 64), 0, stream, a);
+    hipLaunchKernelGGL(weight_apply_kept_kernel<PACK>, dim3((unsigned)((int64_t)a.B * a.apply_blocks * a.Hkv)), dim3(256), 0, stream, a);
+}
+
+template <class K>
+static hipError_t launch_weights_of(const WeightArgs &a, int pack, hipStream_t stream)
+{
+    if (pack == 4) launch_kept<K, 4>(a, stream);
+    else if (pack == 2) launch_kept<K, 2>(a, stream);
+    else if (pack == 1) launch_kept<K, 1>(a, stream);
+    else launch_streamed<K>(a, stream);
     return hipGetLastError();
 }
 
-hipError_t launch_weights(const WeightArgs &a, bool keep, int head_dim, int kv_dtype, hipStream_t stream)
+hipError_t launch_weights(const WeightArgs &a, int pack, int head_dim, int kv_dtype, hipStream_t stream)
 {
-    if (kv_dtype == 0 && head_dim == 128) return launch_weights_of<Bf16Rows<128>>(a, keep, stream);
-    if (kv_dtype == 0 && head_dim == 64) return launch_weights_of<Bf16Rows<64>>(a, keep, stream);
-    if (kv_dtype == 1 && head_dim == 128) return launch_weights_of<Fp8Rows<128>>(a, keep, stream);
-    if (kv_dtype == 1 && head_dim == 64) return launch_weights_of<Fp8Rows<64>>(a, keep, stream);
+    if (kv_dtype == 0 && head_dim == 128) return launch_weights_of<Bf16Rows<128>>(a, pack, stream);
+    if (kv_dtype == 0 && head_dim == 64) return launch_weights_of<Bf16Rows<64>>(a, pack, stream);
+    if (kv_dtype == 1 && head_dim == 128) return launch_weights_of<Fp8Rows<128>>(a, pack, stream);
+    if (kv_dtype == 1 && head_dim == 64) return launch_weights_of<Fp8Rows<64>>(a, pack, stream);
     return hipErrorNotSupported;
 }
 

@@ -133,6 +133,13 @@ DECODE = [  # lens, heads, kv heads, d, kv
     ([20011], 4, 1, 128, "bf16"),                         # several chunks of 64 blocks
     ([130, 700, 0], 40, 2, 64, "bf16"),                  # 20 heads to a KV head: two tiles of rows
     ([90, 600], 64, 1, 128, "fp8"),                       # 64
+    ([6000, 100, 4100], 12, 1, 128, "bf16"),              # 12 heads, long
+    ([9000, 15], 7, 1, 64, "fp8"),
+    ([6500, 3], 8, 2, 64, "bf16"),
+]
+
+MANY = [  # batches of more (sequence, KV head) pairs than half the compute units: a long sequence, many short ones
+    (8192, 16, 2, 64, "bf16"), (8193, 16, 2, 64, "fp8"), (8192, 8, 2, 64, "fp8"), (4096, 24, 2, 64, "bf16"), (4097, 24, 2, 64, "bf16"), (2049, 10, 2, 128, "fp8"), (700, 6, 2, 128, "bf16"),
 ]
 
 
@@ -154,6 +161,16 @@ def test_decode_step(sd, lens, hq, hkv, d, kv, decay):
     again = run(sd, c, hq, q, None, d ** -0.5, decay, 1, before, in_place=True, stride=stride)
     for b, n in enumerate(L):
         assert torch.equal(again[b, :, :n], got[b, :, :n])
+
+
+@pytest.mark.parametrize("longest,hq,hkv,d,kv", MANY)
+def test_many_sequences(sd, longest, hq, hkv, d, kv):
+    rng = np.random.default_rng(longest)
+    lens = rng.integers(0, 60, 86).tolist()
+    lens[7], lens[8], lens[9], lens[50] = 0, longest, 513, longest // 2
+    c = Cache(lens, hkv, d, kv, 11)
+    q = queries(len(lens), hq, d, 12, 2.0)
+    check(run(sd, c, hq, q, None, d ** -0.5), expected(c, q.double().cpu().numpy(), np.arange(len(lens) + 1), lens, d ** -0.5, 1.0, 1, None), lens)
 
 
 WINDOWS = [  # lens, rows of each, heads, kv heads, d, kv
