@@ -482,7 +482,7 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
  * of a smaller one are re-encoded as code * (old / new), fp32, nearest e4m3fn.
  *
  *   sinks, recent      >= 0, sinks + recent <= budget
- *   scores             f32 [batch][num_kv_heads][score_stride], score_stride >= max_context_len
+ *   scores             f32 [batch][num_kv_heads][score_stride]; score_stride at least max_context_len, a multiple of 4
  *   block_table, new_block_table   i32 [batch][max_blocks_per_seq]; of the latter the first
  *                      ceil(min(L, budget) / 16) entries are used.  A new page may be
  *                      neither an old page of the call nor another sequence's new one

@@ -972,7 +972,7 @@ int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recen
     const int rc = check_shape(shape);
     if (rc) return rc;
     if (budget <= 0 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget) return SD_EINVAL;
-    if (score_stride < shape->max_context_len) return SD_EINVAL;
+    if (score_stride < shape->max_context_len || score_stride % 4 != 0) return SD_EINVAL;
     const int32_t most = std::min(budget, shape->max_context_len);   // tokens that stay of a sequence
     if (scores_out && (scores_out_stride < most || (scores_out == scores && scores_out_stride != score_stride))) return SD_EINVAL;
     if (shape->batch == 0) return SD_OK;

@@ -116,6 +116,12 @@ CASES = [  # lens, kv heads, d, kv, budget, sinks, recent
     ([700, 20, 333], 8, 128, "fp8", 100, 7, 50),
     ([5000, 4000, 300], 2, 64, "bf16", 1111, 16, 1000),
     ([70000], 2, 64, "bf16", 4097, 4, 64),               # more than 16 bits of positions
+    ([65536, 65537, 4096], 1, 64, "bf16", 600, 4, 64),
+    ([140000, 5, 66000], 1, 64, "fp8", 70000, 0, 1000),
+    ([4096, 4095, 130], 2, 64, "bf16", 129, 0, 64),
+    ([4097, 4095, 130], 2, 64, "fp8", 129, 1, 64),
+    ([16384, 16383, 8192, 600], 1, 64, "bf16", 511, 4, 64),
+    ([16385, 16383, 8192, 600], 1, 64, "bf16", 511, 4, 64),
     ([300, 200], 2, 128, "fp8", 64, 0, 64),                # nothing left to choose: the last 64
     ([300, 200], 2, 128, "bf16", 64, 64, 0),               # the first
     ([300, 200], 2, 128, "bf16", 64, 20, 44),
@@ -129,9 +135,10 @@ def test_evict(sd, lens, hkv, d, kv, budget, sinks, recent):
     Case(sd, lens, hkv, d, kv, budget, sum(lens) + 1).run_and_check(sd, sinks, recent, in_place=True)
 
 
+@pytest.mark.parametrize("longest", [3000, 9000, 20000])
 @pytest.mark.parametrize("kind", ["equal", "zeros", "few", "nan", "inf", "close", "negative", "ascending", "descending"])
-def test_scores_that_are_hard_to_tell_apart(sd, kind):
-    c = Case(sd, [3000, 130, 1200], 3, 64, "bf16", 128, 77)
+def test_scores_that_are_hard_to_tell_apart(sd, kind, longest):
+    c = Case(sd, [longest, 130, 1200], 3, 64, "bf16", 128, 77)
     rng = np.random.default_rng(1)
     x = c.scores
     if kind == "equal":
@@ -155,6 +162,7 @@ def test_scores_that_are_hard_to_tell_apart(sd, kind):
     else:
         x[:] = -np.arange(x.shape[-1])
     c.run_and_check(sd, 3, 20)
+    c.run_and_check(sd, 0, 0, in_place=True)
 
 
 def test_lengths_outside_the_bound(sd):

@@ -121,7 +121,7 @@ def test_evict_refusals(lib):
     assert evict(lib, s, out=24) == -1
     assert evict(lib, s, budget=0) == -1 and evict(lib, s, sinks=-1) == -1 and evict(lib, s, recent=-1) == -1 and evict(lib, s, sinks=50, recent=51) == -1
     assert evict(lib, s, sinks=2 ** 31 - 1, recent=2 ** 31 - 1) == -1
-    assert evict(lib, s, stride=511) == -1 and evict(lib, s, ostride=99) == -1 and evict(lib, s, out=16, ostride=100) == -1
+    assert evict(lib, s, stride=508) == -1 and evict(lib, s, stride=514) == -1 and evict(lib, s, ostride=99) == -1 and evict(lib, s, out=16, ostride=100) == -1
     assert evict(lib, good_shape(kv_dtype=sd.SD_FP8_E4M3)) == -1
     assert evict(lib, good_shape(head_dim=32)) == -2
     assert evict(lib, good_shape(batch=0), scores=None) == 0
