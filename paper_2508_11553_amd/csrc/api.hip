@@ -752,11 +752,12 @@ bool bad_norm_pointers(const sd_qk_norm *n, const void *q, const void *k, const 
     return bad_ptr(q) || bad_ptr(k) || bad_ptr(q_weight) || bad_ptr(k_weight) || (n->rotary_dim > 0 && (bad_ptr(rope_table) || bad_ptr(positions)));
 }
 
-// Workgroups of the gradient: the queries' rows and the keys' in proportion, about four workgroups to a compute unit of the largest device.
+// Workgroups of the gradient: the queries' rows and the keys' in proportion, four workgroups to a compute unit of the largest device, and two rows to a
+// lane before there are more (16384 tokens, 64/8 heads, with the forward pass: 512 workgroups 272 us, 1024 251, 2048 254; 1531, 16/2 heads: one row 18.0, two 17.1, four 18.2).
 void gradient_blocks(const sd_qk_norm *n, int32_t T, int *q_blocks, int *k_blocks)
 {
     constexpr int64_t kWorkgroups = 2 * kMaxRangeWorkgroups;
-    const int64_t per = 256 / (n->head_dim / 16), heads = (int64_t)n->num_q_heads + n->num_kv_heads;   // rows a workgroup holds at a time
+    const int64_t per = 2 * 256 / (n->head_dim / 16), heads = (int64_t)n->num_q_heads + n->num_kv_heads;
     auto blocks = [&](int64_t h) { return (int)std::max<int64_t>(1, std::min((T * h + per - 1) / per, kWorkgroups * h / heads)); };
     *q_blocks = blocks(n->num_q_heads);
     *k_blocks = blocks(n->num_kv_heads);

@@ -273,6 +273,40 @@ def test_gradient_of_no_rows_and_twice_the_same(sd):
     assert (dqw == 0).all() and (dkw == 0).all()
 
 
+def test_calls_of_many_rows_agree_with_their_halves(sd):
+    """Rows of 64 MB and more stream past the caches: the same rows as from two smaller calls, bit for bit."""
+    import torch
+    T, hq, hkv, d = 4400, 56, 4, 128
+    r = Rows(sd, T, hq, hkv, d, 128, False, 7)
+    dq_out, dk_out = (torch.randn(T, h, d, device="cuda").bfloat16() for h in (hq, hkv))
+    shape = sd.Shape(batch=T, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, page_size=16, num_pages=T, max_blocks_per_seq=1, kv_dtype=sd.SD_BF16, max_context_len=16, chunk_tokens=0)
+    table, slots = torch.randperm(T).int().cuda(), (torch.arange(T) % 16).int().cuda()
+    seq = torch.arange(T, dtype=torch.int32, device="cuda")
+
+    def calls(t0, t1):
+        n = t1 - t0
+        outs = [torch.empty(n, h, d, dtype=torch.bfloat16, device="cuda") for h in (hq, hkv, hq)]
+        pools = [torch.zeros(T, hkv, 16, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        q, k, v, pos = r.q[t0:t1], r.k[t0:t1], r.v[t0:t1], r.positions[t0:t1].clone()
+        sd.qk_norm_rope(r.norm, q, k, r.qw, r.kw, r.table, pos, n, outs[0], outs[1])
+        sd.qk_norm_rope_append(shape, r.norm, q, k, v, r.qw, r.kw, r.table, pos, seq[t0:t1].clone(), slots[t0:t1].clone(), n, outs[2], *pools, table)
+        ws = sd.qk_norm_rope_workspace_bytes(r.norm, n)
+        work, grads, dw = torch.empty(ws, dtype=torch.uint8, device="cuda"), torch.zeros_like(r.all[t0:t1]), [torch.empty(d, device="cuda") for _ in range(2)]
+        sd.qk_norm_rope_backward(r.norm, dq_out[t0:t1], dk_out[t0:t1], q, k, r.qw, r.kw, r.table, pos, n, grads, grads[:, hq * d:], *dw, work, ws)
+        return outs + [grads], pools, dw
+
+    assert T * (hq + hkv) * d * 2 >= 64 << 20
+    rows, pools, dw = calls(0, T)
+    parts = [calls(0, 2000), calls(2000, T)]
+    for i, x in enumerate(rows):
+        assert torch.equal(x, torch.cat([p[0][i] for p in parts]))
+    for i in range(2):
+        assert torch.equal(pools[i], parts[0][1][i] + parts[1][1][i])   # (each half leaves the other's slots 0)
+        want = parts[0][2][i].double() + parts[1][2][i].double()
+        _, _, size = backward(f64((dq_out, dk_out)[i]), r.host((r.q, r.k)[i], (hq, hkv)[i]), f64((r.qw, r.kw)[i]), *r.rest())
+        assert (np.abs(f64(dw[i]) - want.cpu().numpy()) <= 2 * 114 * U * size).all()
+
+
 def test_another_stream(sd):
     import torch
     r = Rows(sd, 50, 8, 2, 128, 128, False, 8)

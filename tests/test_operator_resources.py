@@ -11,7 +11,7 @@ from tests.test_kernel_resources import resource_remarks
 
 @pytest.mark.skipif(shutil.which(sd_build.HIPCC) is None and not os.path.exists(sd_build.HIPCC), reason="needs hipcc")
 @pytest.mark.parametrize("source,least", [
-    ("norm_rope.hip", {"norm_rope_kernel": (4, 4), "norm_rope_backward_kernel": (2, 4), "norm_weight_kernel": (2, 4)}),
+    ("norm_rope.hip", {"norm_rope_kernel": (8, 4), "norm_rope_backward_kernel": (4, 4), "norm_weight_kernel": (2, 4)}),
     # 16 waves of one workgroup at four to a SIMD; 8 of two workgroups
     ("weight_scores.hip", {"weight_whole_kernel": (12, 4), "weight_products_kernel": (12, 4), "weight_apply_kept_kernel": (3, 4), "weight_stats_kernel": (4, 4),
                            "weight_apply_kernel": (4, 4), "weight_rows_kernel": (1, 4)}),
