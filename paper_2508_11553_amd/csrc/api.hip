@@ -798,8 +798,10 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
         const int64_t pages = parts(tokens, sd::kPage);
         w.wave_tiles = std::max<int64_t>(parts(units * pages > 5000 ? 4 : 2, w.pack), parts(pages, 128 * sd::kWaves * w.pack));
     } else {
-        // Groups of four pages: as many workgroups as run at once, or a multiple (8 sequences of 5 k - 8 k, 8 KV heads, 256 rows: 16 groups 86, 8 97, 4 92).
-        const int64_t groups = units * parts(tokens, 4 * sd::kPage), slots = kMaxRangeWorkgroups;
+        // Groups of four pages: as many workgroups as run at once, or a multiple.  Of eight waves two fit a compute unit, of up to four four (us with 512 : 1024
+        // workgroups: 256 rows, 8 sequences of 5 k - 8 k, 8 KV heads 92 : 102, two of 1 k - 4 k 27 : 36; 16 of 1 k - 4 k: 32 rows 49 : 41, fp8 48 : 32, 64 rows 52 : 43,
+        // 128 rows 56 : 55, head_dim 64 45 : 42).
+        const int64_t groups = units * parts(tokens, 4 * sd::kPage), slots = kMaxRangeWorkgroups / 2 * std::min(4, 16 / sd::row_waves(w.rows));
         w.wave_tiles = std::max<int64_t>(1, parts(groups, slots * parts(groups, slots * sd::kMaxGroups)));
     }
     w.block_tokens = sd::kPage * w.wave_tiles * (w.pack ? sd::kWaves * w.pack : 4);

@@ -636,6 +636,13 @@ struct NormGradArgs {
 
 // Attention weights into running scores (weight_scores.hip).
 constexpr int kMaxGroups = 16;    // groups of four pages that a workgroup walks where the products are made twice
+constexpr int kRowsOfWave = 32, kRowWaves = 8;   // rows that a wave holds there, waves of a workgroup at most
+// As many waves as share the rows alike: 800 rows are four rounds of seven waves (98 us, three of eight and one of one 100).
+constexpr int row_waves(int64_t rows)
+{
+    const int64_t shares = rows <= kRowsOfWave ? 1 : (rows + kRowsOfWave - 1) / kRowsOfWave, rounds = (shares + kRowWaves - 1) / kRowWaves;
+    return (int)((shares + rounds - 1) / rounds);
+}
 constexpr int whole_tiles(int pack) { return pack == 4 ? 8 : 16; }   // tiles of products that a wave's registers hold where both steps are one
 // Pages that share a tile of products, of at most 16 rows.
 constexpr int weight_pack(int64_t rows) { return rows <= 4 ? 4 : rows <= 8 ? 2 : 1; }

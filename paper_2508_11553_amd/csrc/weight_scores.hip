@@ -389,7 +389,7 @@ __global__ __launch_bounds__(1024) void weight_whole_kernel(WeightArgs a)
 // kGroupPages pages of one (sequence, KV head), once for every kRowTiles * 16 * waves rows; its waves bring a group into LDS, a page
 // each, and all read it as operands, kAtOnce pages at a time, while the next one comes.
 constexpr int kGroupPages = 4, kGroupTokens = kGroupPages * kPage, kAtOnce = 2;
-constexpr int kRowTiles = 2, kRowsOfWave = kRowTiles * kMaxGroup, kRowWaves = 8;
+constexpr int kRowTiles = kRowsOfWave / kMaxGroup;
 template <class K>
 struct Stream {
     static constexpr int S = K::kDim / 32;
@@ -627,7 +627,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
 template <class K>
 static void launch_streamed(const WeightArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((int64_t)a.B * a.blocks * a.Hkv)), block(std::max(1, std::min(kRowWaves, (a.max_rows + kRowsOfWave - 1) / kRowsOfWave)) * 64);
+    const dim3 grid((unsigned)((int64_t)a.B * a.blocks * a.Hkv)), block(row_waves(a.max_rows) * 64);
     hipLaunchKernelGGL(weight_stats_kernel<K>, grid, block, 0, stream, a);
     if (a.row_blocks) hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)((int64_t)a.B * a.Hkv * a.row_blocks)), dim3(256), 0, stream, a);
     hipLaunchKernelGGL(weight_apply_kernel<K>, grid, block, block.x / 64 * a.block_tokens * 4, stream, a);
