@@ -809,8 +809,11 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
     w.tiles = w.pack ? parts(tokens, w.pack * sd::kPage) : 0;
     w.apply_blocks = parts(tokens, 1024);
     w.row_blocks = parts(w.rows, 64);
+    // The workspace is that of the most blocks, and of kept products though one kernel may do without: a caller's, sized for its largest batch
+    // and longest sequences, serves every smaller call.
+    const int64_t most_blocks = parts(tokens, w.pack ? sd::kPage * sd::kWaves * w.pack * parts(2, w.pack) : 4 * sd::kPage);
     w.stats_off = up((size_t)units * w.tiles * 1024);
-    w.rows_off = w.stats_off + up((size_t)units * w.blocks * (w.pack ? sd::kMaxGroup / w.pack : w.rows) * 8);
+    w.rows_off = w.stats_off + up((size_t)units * most_blocks * (w.pack ? sd::kMaxGroup / w.pack : w.rows) * 8);
     w.total = w.rows_off + (w.pack ? 0 : up((size_t)units * w.rows * 8));
     return w;
 }

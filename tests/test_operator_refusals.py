@@ -109,6 +109,16 @@ def test_weight_refusals(lib):
     assert sd.paged_weight_workspace_bytes(s, 64) > 0
 
 
+@pytest.mark.parametrize("heads,most", [(4, 1), (8, 1), (16, 1), (64, 1), (8, 3), (16, 40)])
+def test_weight_workspace_of_a_large_call_serves_the_smaller(heads, most):
+    sizes = [[sd.paged_weight_workspace_bytes(good_shape(batch=b, num_q_heads=heads, num_kv_heads=2, max_blocks_per_seq=8192, max_context_len=n), most)
+              for n in (0, 1, 100, 1000, 1023, 4096, 5000, 9000, 70000, 131072)] for b in (1, 2, 13, 40, 79, 80, 81, 200, 499, 500, 1000)]
+    for x, y in zip(sizes, sizes[1:]):
+        assert all(0 < i <= j for i, j in zip(x, y))
+    for x in sizes:
+        assert x == sorted(x)
+
+
 def evict(lib, shape, budget=100, sinks=4, recent=20, scores=16, stride=512, kp=32, vp=48, ks=None, vs=None, bt=64, lens=80, nbt=96, kept=112, nl=128, out=144, ostride=100):
     return lib.kv_evict(ctypes.byref(shape), budget, sinks, recent, scores, stride, kp, vp, ks, vs, bt, lens, nbt, kept, nl, out, ostride, None)
 
