@@ -122,6 +122,8 @@ struct Stat {
     float m, l;   // maximum (log2 domain) and sum of exp2(x - m)
 };
 SD_DEV float shrink_of(float from, float to) { return from == to ? 1.f : __builtin_amdgcn_exp2f(from - to); }   // (both may be -inf)
+// What exponents are taken relative to: not a maximum of -inf, which is all that a stretch of tokens without any weight has.
+SD_DEV float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
 SD_DEV Stat joined(Stat x, Stat y)
 {
     const float m = fmaxf(x.m, y.m);
@@ -225,10 +227,11 @@ __global__ __launch_bounds__(kWaves * 64) void weight_products_kernel(WeightArgs
         float m = stat.m;
 #pragma unroll
         for (int e = 0; e < 4; ++e) m = fmaxf(m, t0 + e < end ? x[e] : -INFINITY);
+        const float ref = reference_of(m);
         float l = stat.l * shrink_of(stat.m, m);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[e] - m);
+            const float p = __builtin_amdgcn_exp2f(x[e] - ref);
             l += t0 + e < end ? p : 0.f;
         }
         stat = Stat{m, l};
@@ -299,15 +302,15 @@ __global__ __launch_bounds__(256) void weight_apply_kept_kernel(WeightArgs a)
 #pragma unroll
     for (int i = 0; i < T; ++i) {
         if (tile0 + i < tiles) {   // wave-uniform
-        float sum = 0.f;
+            float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[i][e] - row.x) * row.y;
-            const float all = over_rows<W>(t0 + i * PACK * kPage + e < end ? p : 0.f);
-            sum = at.row == e ? all : sum;
-        }
-        const int t = mine + i * PACK * kPage;
-        if (at.row < 4 && t < s.L) a.scores_out[scores + t] = sum + a.decay * before[i];
+            for (int e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(x[i][e] - row.x) * row.y;
+                const float all = over_rows<W>(t0 + i * PACK * kPage + e < end ? p : 0.f);
+                sum = at.row == e ? all : sum;
+            }
+            const int t = mine + i * PACK * kPage;
+            if (at.row < 4 && t < s.L) a.scores_out[scores + t] = sum + a.decay * before[i];
         }
     }
 }
@@ -346,6 +349,7 @@ __global__ __launch_bounds__(1024) void weight_whole_kernel(WeightArgs a)
         for (int e = 0; e < 4; ++e) m = fmaxf(m, t0 + e < end ? x[i][e] : -INFINITY);
     }
     for (int off = W; off < 64; off *= 2) m = fmaxf(m, __shfl_xor(m, off, 64));
+    const float ref = reference_of(m);
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < T; ++i) {
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(1024) void weight_whole_kernel(WeightArgs a)
         if (tile >= tiles) break;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            x[i][e] = __builtin_amdgcn_exp2f(x[i][e] - m);
+            x[i][e] = __builtin_amdgcn_exp2f(x[i][e] - ref);
             if (tile * PACK * kPage + at.token() + e >= end) x[i][e] = 0.f;
             l += x[i][e];
         }
@@ -487,12 +491,13 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
                                 for (int e = 0; e < 4; ++e) x[p][e] = 16 * p + e < end ? x[p][e] * scale[p] : -INFINITY;
                             m = max_of(m, by[p] * max_of(max_of(x[p][0], x[p][1]), x[p][2], x[p][3]));
                         }
+                        const float ref = reference_of(m);
                         float l = stat[i].l * shrink_of(stat[i].m, m);
 #pragma unroll
                         for (int p = 0; p < kAtOnce; ++p)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], by[p], -m));
+                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], by[p], -ref));
                                 l += !masked || 16 * p + e < end ? w : 0.f;
                             }
                         stat[i] = Stat{m, l};

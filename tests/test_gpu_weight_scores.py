@@ -244,6 +244,43 @@ def test_a_score_that_is_not_finite_stays_in_its_head(sd, starts):
     assert got[0, 0, 53] == 0 and got[0, 0].isfinite().all()
 
 
+@pytest.mark.parametrize("lens,hq,hkv,d,starts", [([700], 8, 2, 64, None), ([6000], 4, 1, 128, None), ([5000], 8, 1, 64, None), ([4500], 12, 1, 64, None),
+                                                  ([900], 8, 2, 64, [0, 40]), ([900], 8, 2, 128, [0, 3]), ([300, 20] * 40, 8, 2, 64, None)])
+def test_stretches_of_tokens_without_any_weight(sd, lens, hq, hkv, d, starts):
+    """Keys whose scores are -inf, single ones, whole pages, the first and the last of a sequence: weight 0, and the others' weights as if
+    those tokens were not there.  A row that has nothing else is NaN (0 / 0), as the definition is."""
+    c = Cache(lens, hkv, d, "bf16", 21)
+    L = lens[0]
+    gone = np.zeros(L, bool)
+    gone[:67] = gone[90:112] = gone[113] = gone[130:134] = gone[L // 2:L // 2 + 70] = True
+    for t in np.flatnonzero(gone):
+        c.pool[int(c.table[0, t // 16]), 0, t % 16, 3] = float("-inf")
+    n = len(lens) if starts is None else starts[-1]
+    q = queries(n, hq, d, 22)
+    q[..., 3] = 0.5
+    got = run(sd, c, hq, q, starts, d ** -0.5)[0].double().cpu().numpy()
+    k, G = c.k[0][:, 0].copy(), hq // hkv
+    k[gone, 3] = 0
+    want, tol = np.zeros(L), np.zeros(L)
+    rows = q.double().cpu().numpy()[:1 if starts is None else n]
+    for i, row in enumerate(rows):
+        end = L - len(rows) + 1 + i
+        for h in range(G):
+            x = np.where(gone[:end], -np.inf, d ** -0.5 * (k[:end] @ row[h]))
+            size = d ** -0.5 * (np.abs(k[:end]) @ np.abs(row[h])).max()
+            p = np.exp(x - x.max())
+            want[:end] += p / p.sum()
+            tol[:end] += p / p.sum() * (3 * (d + 4) * size * U + (64 + size) * 2 * U) + 1e-37
+    assert (got[0, :L][gone] == 0).all()
+    assert (np.abs(got[0, :L] - want) <= tol + want * 80 * U).all()
+    if hkv > 1:
+        assert (got[1, :L] > 0).all()
+    for t in range(L):
+        c.pool[int(c.table[0, t // 16]), 0, t % 16, 3] = float("-inf")
+    got = run(sd, c, hq, q, starts, d ** -0.5)[0]
+    assert got[0, :L].isnan().all() and (hkv == 1 or got[1, :L].isfinite().all())
+
+
 def test_weights_of_a_decode_step_sum_to_the_heads(sd):
     """Every row's weights sum to one: the scores of a KV head to its query heads, whatever the lengths."""
     lens = [1, 7, 4000, 16383]
