@@ -1,0 +1,53 @@
+"""Host arithmetic of the operators around the decode step (CPU only: compiled from kernels.h for the host)."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2508_11553_amd import build as sd_build
+from tests.test_kernel_resources import CSRC
+
+PROGRAM = r'''
+#include <cstdio>
+#include <cstdlib>
+#include "kernels.h"
+static void fail(const char *what, unsigned long a, unsigned long b) { std::printf("%s %lu %lu\n", what, a, b); std::exit(1); }
+int main()
+{
+    // division by a product: every divisor a call can bring, at the numerators next to its multiples and at the largest
+    unsigned long state = 1;
+    for (unsigned by = 1; by <= 5000; ++by) {
+        const sd::Division d = sd::division_by(by);
+        for (int i = 0; i < 200; ++i) {
+            state = state * 6364136223846793005ul + 1442695040888963407ul;
+            const unsigned x = (unsigned)(state >> 33), q = x / by * by;   // below 2^31
+            for (unsigned y : {x, q, q ? q - 1 : 0u, 0x7fffffffu, 0x7fffffffu / by * by, 0u, by - 1, by < 0x7fffffffu ? by : 0u})
+                if (d.of(y) != y / by) fail("division", y, by);
+        }
+    }
+    for (unsigned by : {1u << 20, (1u << 20) + 1, 0x3fffffffu, 0x40000000u, 0x7ffffffeu, 0x7fffffffu})
+        for (unsigned y : {0u, by - 1, by, 0x7fffffffu, 0x7ffffffeu, 12345u})
+            if (sd::division_by(by).of(y) != y / by) fail("division", y, by);
+    // tiles of products have room for the rows; waves for all rows in as few rounds as the most waves need
+    for (long rows = 1; rows <= 16; ++rows)
+        if (16 / sd::weight_pack(rows) < rows || (sd::weight_pack(rows) < 4 && 16 / (2 * sd::weight_pack(rows)) >= rows)) fail("pack", rows, sd::weight_pack(rows));
+    for (long rows = 0; rows <= 5000; ++rows) {
+        const int waves = sd::row_waves(rows);
+        if (waves < 1 || waves > sd::kRowWaves) fail("waves", rows, waves);
+        const auto rounds = [rows](int w) { return (rows + w * sd::kRowsOfWave - 1) / (w * sd::kRowsOfWave); };
+        if (rounds(waves) != rounds(sd::kRowWaves) || (waves > 1 && rounds(waves - 1) == rounds(waves))) fail("rounds", rows, waves);
+    }
+    std::printf("ok");
+}
+'''
+
+
+@pytest.mark.skipif(shutil.which(sd_build.HIPCC) is None and not os.path.exists(sd_build.HIPCC), reason="needs hipcc")
+def test_rules_compiled_for_the_host(tmp_path):
+    (tmp_path / "rules.hip").write_text(PROGRAM)
+    r = subprocess.run([sd_build.HIPCC, "--offload-host-only", "-O1", "-std=c++17", f"-I{CSRC}", str(tmp_path / "rules.hip"), "-o", str(tmp_path / "rules")],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    out = subprocess.run([str(tmp_path / "rules")], capture_output=True, text=True)
+    assert out.returncode == 0 and out.stdout == "ok", out.stdout
