@@ -794,9 +794,9 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
     }
     if (w.pack) {
         // A wave's pages: two while that makes no more than 2500 waves, else four (32 units of 4096 14.7 : 13.9, 64 of 1200 12.2 : 12.6); and
-        // no more than 128 workgroups to a sequence, whose statistics every workgroup of the second step reads.
+        // no more than 128 workgroups to a sequence, whose statistics every workgroup of the second step reads, but at most 64 pages, whose ids its lanes hold.
         const int64_t pages = parts(tokens, sd::kPage);
-        w.wave_tiles = std::max<int64_t>(parts(units * pages > 5000 ? 4 : 2, w.pack), parts(pages, 128 * sd::kWaves * w.pack));
+        w.wave_tiles = std::max<int64_t>(parts(units * pages > 5000 ? 4 : 2, w.pack), std::min<int64_t>(parts(pages, 128 * sd::kWaves * w.pack), 64 / w.pack));
     } else {
         // Groups of four pages: as many workgroups as run at once, or a multiple.  Of eight waves two fit a compute unit, of up to four four (us with 512 : 1024
         // workgroups: 256 rows, 8 sequences of 5 k - 8 k, 8 KV heads 92 : 102, two of 1 k - 4 k 27 : 36; 16 of 1 k - 4 k: 32 rows 49 : 41, fp8 48 : 32, 64 rows 52 : 43,

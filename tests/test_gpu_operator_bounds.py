@@ -1,0 +1,47 @@
+"""The operators around the decode step at the ends of their ranges: very long sequences, loose bounds on the query rows, large budgets."""
+import pytest
+
+from tests.test_gpu_operator_reach import shape_of
+from tests.test_gpu_weight_scores import U, queries
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sd():
+    import torch
+    assert torch.cuda.is_available()
+    import paper_2508_11553_amd as m
+    m.load()
+    return m
+
+
+def weights_of(q, k, scale):
+    """-> sums of the rows' weights over k [L][d] and their tolerances (derived in test_gpu_weight_scores), q [rows][d]; 64 bits"""
+    x = scale * (q @ k.T)
+    size = abs(scale) * (q.abs() @ k.abs().T).amax(1, keepdim=True)
+    p = (x - x.amax(1, keepdim=True)).exp()
+    p /= p.sum(1, keepdim=True)
+    tol = (p * (3 * (k.shape[1] + 4) * size * U + (64 + x.abs().amax(1, keepdim=True)) * 2 * U) + 1e-37).sum(0)
+    return p.sum(0), tol + p.sum(0) * 80 * U
+
+
+@pytest.mark.parametrize("heads", [4, 8, 16, 32])
+@pytest.mark.parametrize("L", [524288, 600001, 1100000])
+def test_weights_of_more_than_half_a_million_tokens(sd, heads, L):
+    """A wave of the first step takes as many pages as it has lanes, and then there are more workgroups.  Every page of a small pool many times."""
+    import torch
+    d, pages, blocks = 64, 500, (L + 15) // 16
+    gen = torch.Generator().manual_seed(heads)
+    pool = torch.randn(pages, 1, 16, d, generator=gen).bfloat16().cuda()
+    table = torch.randint(0, pages, (1, blocks), generator=gen, dtype=torch.int32).cuda()
+    q = queries(1, heads, d, 3)
+    shape = shape_of(sd, 1, heads, 1, d, pages, blocks, L)
+    stride = (L + 3) // 4 * 4
+    out = torch.full((stride,), float("nan"), device="cuda")
+    ws = sd.paged_weight_workspace_bytes(shape, 1)
+    work = torch.empty(ws, dtype=torch.uint8, device="cuda").fill_(255)
+    sd.paged_weight_accumulate(shape, q, None, 1, 1, pool, None, table, torch.tensor([L], dtype=torch.int32, device="cuda"), d ** -0.5, 1.0, 0, None, out, stride, work, ws)
+    k = pool[:, 0].double()[table[0].long()].reshape(-1, d)[:L]
+    want, tol = weights_of(q[0].double(), k, d ** -0.5)
+    assert bool(((out[:L].double() - want).abs() <= tol).all())
