@@ -457,8 +457,8 @@ int qk_norm_rope_backward(const sd_qk_norm *norm, const void *dq_out, const void
  *   scores_out   f32, the same layout; entries at positions >= L are left as they are
  *   score_stride at least max_context_len, a multiple of 4
  *   workspace    >= paged_weight_workspace_bytes(shape, max_q_len) bytes, contents ignored; never less for a
- *                larger batch or max_context_len.  Up to 16 query rows for a KV head (max_q_len times the heads of
- *                its group) it holds 4 bytes per row and token of the bound, rows counted as 4, 8 or 16
+ *                larger batch, max_context_len or max_q_len.  It holds 4 bytes per row and token of the bound, rows
+ *                (max_q_len times the heads of a group) counted as 4, 8 or 16, and what more rows need if that is more
  */
 size_t paged_weight_workspace_bytes(const sd_shape *shape, int32_t max_q_len);
 int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t *q_start,

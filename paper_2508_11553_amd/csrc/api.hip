@@ -809,12 +809,18 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
     w.tiles = w.pack ? parts(tokens, w.pack * sd::kPage) : 0;
     w.apply_blocks = parts(tokens, 1024);
     w.row_blocks = parts(w.rows, 64);
-    // The workspace is that of the most blocks, and of kept products though one kernel may do without: a caller's, sized for its largest batch
-    // and longest sequences, serves every smaller call.
-    const int64_t most_blocks = parts(tokens, w.pack ? sd::kPage * sd::kWaves * w.pack * parts(2, w.pack) : 4 * sd::kPage);
-    w.stats_off = up((size_t)units * w.tiles * 1024);
-    w.rows_off = w.stats_off + up((size_t)units * most_blocks * (w.pack ? sd::kMaxGroup / w.pack : w.rows) * 8);
-    w.total = w.rows_off + (w.pack ? 0 : up((size_t)units * w.rows * 8));
+    // The workspace is that of the most blocks, and of kept products though one kernel may do without or there are too many rows: a caller's, sized
+    // for its largest batch, longest sequences and most query rows, serves every smaller call.
+    const auto layout = [&](int64_t rows) {
+        const int pack = rows <= sd::kMaxGroup ? sd::weight_pack(rows) : 0;
+        const int64_t most_blocks = parts(tokens, pack ? sd::kPage * sd::kWaves * pack * parts(2, pack) : 4 * sd::kPage);
+        w.stats_off = pack ? up((size_t)units * parts(tokens, pack * sd::kPage) * 1024) : 0;
+        w.rows_off = w.stats_off + up((size_t)units * most_blocks * (pack ? sd::kMaxGroup / pack : rows) * 8);
+        return w.rows_off + (pack ? 0 : up((size_t)units * rows * 8));
+    };
+    const int64_t group = s->num_q_heads / s->num_kv_heads;
+    const size_t fewer = layout(std::min(w.rows, sd::kMaxGroup / group * group));
+    w.total = std::max(layout(w.rows), fewer);
     return w;
 }
 

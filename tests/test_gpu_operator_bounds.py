@@ -45,3 +45,34 @@ def test_weights_of_more_than_half_a_million_tokens(sd, heads, L):
     k = pool[:, 0].double()[table[0].long()].reshape(-1, d)[:L]
     want, tol = weights_of(q[0].double(), k, d ** -0.5)
     assert bool(((out[:L].double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(8, 2), (16, 1), (32, 1)])
+@pytest.mark.parametrize("total", [0, 1, 2, 5])
+def test_a_bound_on_the_query_rows_that_few_rows_come_near(sd, heads, kv_heads, total):
+    """The bytes that the bound asks for serve a call of fewer rows, which may take another path."""
+    import torch
+    d, L, most = 64, [3000, 41], 40
+    blocks = (max(L) + 15) // 16
+    gen = torch.Generator().manual_seed(total)
+    pool = torch.randn(2 * blocks, kv_heads, 16, d, generator=gen).bfloat16().cuda()
+    table = torch.randperm(2 * blocks, generator=gen).view(2, blocks).int().cuda()
+    shape = shape_of(sd, 2, heads, kv_heads, d, 2 * blocks, blocks, max(L))
+    q = queries(max(total, 1), heads, d, 8)
+    first = total // 2
+    starts = torch.tensor([0, first, total], dtype=torch.int32, device="cuda")
+    before = torch.rand(2, kv_heads, max(L), device="cuda")
+    out = torch.full_like(before, float("nan"))
+    ws = sd.paged_weight_workspace_bytes(shape, most)
+    work = torch.empty(ws, dtype=torch.uint8, device="cuda").fill_(255)
+    sd.paged_weight_accumulate(shape, q, starts, total, most, pool, None, table, torch.tensor(L, dtype=torch.int32, device="cuda"), d ** -0.5, 0.5, 0, before, out, max(L), work, ws)
+    for b, (lo, hi) in enumerate(((0, first), (first, total))):
+        k = pool.double()[table[b].long()].transpose(1, 2).reshape(-1, kv_heads, d)[:L[b]]
+        for g in range(kv_heads):
+            want, tol = 0.5 * before[b, g, :L[b]].double(), 8 * U * torch.ones(L[b], dtype=torch.float64, device="cuda")
+            for i in range(lo, hi):
+                end, rows = L[b] - hi + i + 1, q[i, g * (heads // kv_heads):(g + 1) * (heads // kv_heads)].double()
+                p, t = weights_of(rows, k[:end, g].contiguous(), d ** -0.5)
+                want[:end] += p
+                tol[:end] += t
+            assert bool(((out[b, g, :L[b]].double() - want).abs() <= tol + 8 * U * want).all()), (b, g)

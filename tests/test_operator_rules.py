@@ -51,3 +51,14 @@ def test_rules_compiled_for_the_host(tmp_path):
     assert r.returncode == 0, r.stderr[-2000:]
     out = subprocess.run([str(tmp_path / "rules")], capture_output=True, text=True)
     assert out.returncode == 0 and out.stdout == "ok", out.stdout
+
+
+@pytest.mark.parametrize("heads", [2, 6, 8, 24, 64])
+def test_weight_workspace_of_many_rows_serves_fewer(heads):
+    import paper_2508_11553_amd as sd
+    from tests.test_abi import good_shape
+    for n in (1, 500, 5000, 131072):
+        for batch in (1, 16, 300):
+            s = good_shape(batch=batch, num_q_heads=heads, num_kv_heads=2, max_blocks_per_seq=8192, max_context_len=n)
+            sizes = [sd.paged_weight_workspace_bytes(s, most) for most in range(70)]
+            assert 0 < sizes[0] and sizes == sorted(sizes)
