@@ -720,7 +720,13 @@ int check_norm(const sd_qk_norm *n)
     return SD_OK;
 }
 
-bool too_many_rows(const sd_qk_norm *n, int32_t T) { return (uint64_t)T * ((uint64_t)n->num_q_heads + 2 * (uint64_t)n->num_kv_heads) > sd::kMaxRows; }
+bool too_many_threads(uint64_t workgroups, uint64_t threads) { return workgroups > sd::kMaxThreads / threads; }
+
+// (rows of T tokens; the last workgroup may be partly empty)
+bool too_many_rows(const sd_qk_norm *n, int32_t T)
+{
+    return (uint64_t)T * ((uint64_t)n->num_q_heads + 2 * (uint64_t)n->num_kv_heads) > (sd::kMaxThreads - 256) / (uint64_t)(n->head_dim / 16);
+}
 
 sd::NormRopeArgs norm_args(const sd_qk_norm *n, const void *q, const void *k, const void *q_weight, const void *k_weight, const float *rope_table,
                            const int32_t *positions, int32_t T, void *q_out, void *k_out)
@@ -934,8 +940,10 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
         return SD_EINVAL;
     if (shape->kv_dtype == SD_FP8_E4M3 && bad_ptr(k_scales)) return SD_EINVAL;
     max_q_len = std::min(max_q_len, total_q);
+    const uint64_t units = (uint64_t)shape->batch * shape->num_kv_heads;
+    if (too_many_threads(units, 1024)) return SD_EUNSUPPORTED;
     const WeightPlan w = weight_plan(shape, max_q_len);
-    if (w.rows > 0x7fffffff || (int64_t)shape->batch * shape->num_kv_heads * std::max({w.blocks, w.apply_blocks, w.row_blocks}) > 0x7fffffff) return SD_EUNSUPPORTED;
+    if (w.rows > 0x7fffffff || too_many_threads(units * std::max({w.blocks, w.apply_blocks, w.row_blocks}), 512)) return SD_EUNSUPPORTED;
     if (workspace_bytes < w.total) return SD_EWORKSPACE;
     char *ws = static_cast<char *>(workspace);
     sd::WeightArgs a;
@@ -1015,7 +1023,8 @@ int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recen
     a.sinks = sinks;
     a.recent = recent;
     a.new_pages = std::max(1, (most + sd::kPage - 1) / sd::kPage);
-    if ((int64_t)a.B * a.Hkv * a.new_pages > 0x7fffffff) return SD_EUNSUPPORTED;
+    const uint64_t units = (uint64_t)a.B * a.Hkv;
+    if (too_many_threads(units, 1024) || too_many_threads(units * a.new_pages, 64)) return SD_EUNSUPPORTED;   // the choice, the move
     const hipError_t e = sd::launch_evict(a, shape->head_dim, shape->kv_dtype, static_cast<hipStream_t>(stream));
     if (e == hipErrorNotSupported) return SD_EUNSUPPORTED;
     return e == hipSuccess ? SD_OK : hip_fail(e);

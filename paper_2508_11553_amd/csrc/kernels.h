@@ -601,7 +601,7 @@ __host__ inline Division division_by(uint32_t by)
     while (((uint64_t)1 << l) < by) ++l;
     return Division{(uint32_t)((((uint64_t)1 << (31 + l)) / by) + 1), (uint32_t)(l - 1)};
 }
-constexpr uint64_t kMaxRows = 0x7fffffff;   // head rows of one call: half a terabyte of them
+constexpr uint64_t kMaxThreads = 0xffffffff;   // of one launch
 
 // Rows of the norm and rotation (norm_rope.hip): x rows of q and k at strides, y rows contiguous.
 struct NormRopeArgs {

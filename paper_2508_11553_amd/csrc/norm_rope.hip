@@ -282,7 +282,6 @@ hipError_t launch_norm_rope(const NormRopeArgs &n, const RowPages *pages, int he
 {
     const uint32_t rows = n.Hq + (pages ? 2 : 1) * n.Hkv;
     if (n.T <= 0) return hipSuccess;
-    if ((uint64_t)n.T * rows > kMaxRows) return hipErrorNotSupported;
     RowPages p = {};
     if (pages) p = *pages;
     p.per_token = division_by(rows);

@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from paper_2508_11553_amd import build as sd_build
+from tests.test_abi import lib  # noqa: F401
 from tests.test_kernel_resources import CSRC
 
 PROGRAM = r'''
@@ -62,3 +63,19 @@ def test_weight_workspace_of_many_rows_serves_fewer(heads):
             s = good_shape(batch=batch, num_q_heads=heads, num_kv_heads=2, max_blocks_per_seq=8192, max_context_len=n)
             sizes = [sd.paged_weight_workspace_bytes(s, most) for most in range(70)]
             assert 0 < sizes[0] and sizes == sorted(sizes)
+
+
+def test_calls_of_more_threads_than_a_launch_has(lib):
+    """2^32 - 1 threads: a launch of more fails, and one that follows it would read what the first has not written."""
+    from tests.test_abi import good_shape
+    from tests.test_operator_refusals import append, evict, good_norm, gradient, rows, weights
+    for d, T in ((64, 2 ** 30 // 12 + 1), (128, 2 ** 29 // 12 + 1)):      # d / 16 threads to a row, 12 rows to a token
+        n, s = good_norm(head_dim=d), good_shape(head_dim=d)
+        assert rows(lib, n, T=T) == -2 and append(lib, s, n, T=T) == -2 and gradient(lib, n, T=T) == -2
+    assert evict(lib, good_shape(batch=2 ** 21, num_kv_heads=2)) == -2                    # 1024 to a (sequence, KV head)
+    assert evict(lib, good_shape(batch=2 ** 14, num_kv_heads=2, max_blocks_per_seq=8192, max_context_len=131072), budget=131072, stride=131072, ostride=131072) == -2   # 64 to a page
+    assert evict(lib, good_shape(batch=2 ** 31 - 1, num_q_heads=2 ** 31 - 1, num_kv_heads=2 ** 31 - 1)) == -2
+    assert weights(lib, good_shape(batch=2 ** 21, num_kv_heads=2), total=2 ** 21) == -2
+    assert weights(lib, good_shape(batch=2 ** 31 - 1, num_q_heads=2 ** 31 - 1, num_kv_heads=2 ** 31 - 1), total=2 ** 31 - 1) == -2
+    long = good_shape(batch=2 ** 18, num_q_heads=64, num_kv_heads=2, max_blocks_per_seq=8192, max_context_len=131072)
+    assert weights(lib, long, qs=32, total=2 ** 19, most=2, stride=131072, size=2 ** 60) == -2
