@@ -198,7 +198,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
         more = s_found[0];
         equal = s_found[1];
     }
-    for (int i = stay + tid; i < a.budget; i += THREADS) kept[i] = -1;
+    for (unsigned i = stay + tid; i < (unsigned)a.budget; i += THREADS) kept[i] = -1;   // (a budget may be the largest int)
 }
 
 // One new (page, head) tile of K or of V by one wave.  Row r comes from row `from` (of lane r) of the pool; rows past the n-th are left alone.

@@ -76,3 +76,17 @@ def test_a_bound_on_the_query_rows_that_few_rows_come_near(sd, heads, kv_heads, 
                 want[:end] += p
                 tol[:end] += t
             assert bool(((out[b, g, :L[b]].double() - want).abs() <= tol + 8 * U * want).all()), (b, g)
+
+
+def test_the_largest_budget(sd):
+    """2^31 - 1 places, of which a sequence fills 300."""
+    import torch
+    hkv, d, L, budget, blocks = 1, 64, 300, 2 ** 31 - 1, 19
+    pools = [torch.randn(2 * blocks, hkv, 16, d, device="cuda").bfloat16() for _ in range(2)]
+    old = pools[0][:blocks].clone()
+    table, new = (torch.arange(i * blocks, (i + 1) * blocks, dtype=torch.int32, device="cuda").view(1, blocks) for i in range(2))
+    lens, new_lens = torch.tensor([L], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    kept = torch.zeros(budget, dtype=torch.int32, device="cuda")
+    sd.kv_evict(shape_of(sd, 1, 4, hkv, d, 2 * blocks, blocks, L), budget, 4, 20, torch.rand(1, hkv, L, device="cuda"), L, *pools, None, None, table, lens, new, kept, new_lens)
+    assert torch.equal(kept[:L], torch.arange(L, dtype=torch.int32, device="cuda")) and int(kept[L:].max()) == int(kept[L:].min()) == -1
+    assert int(new_lens) == L and torch.equal(pools[0][blocks:].view(-1, d)[:L], old.view(-1, d)[:L])
