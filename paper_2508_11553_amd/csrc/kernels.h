@@ -656,7 +656,7 @@ struct WeightArgs {
     float *scores_out;
     float *products;                     // [B][Hkv][max_tiles][64 lanes][4]: a decode step's, log2 domain
     float2 *stats;                       // (max, sum) of a row over a stretch of tokens.  Products kept: [B][Hkv][blocks][16 / pack], else [B][Hkv][blocks][max_rows]
-    float2 *rows;                        // [B][Hkv][max_rows]: (max, 1 / sum) of a row
+    float *rows;                         // [B][Hkv][max_rows]: log2 of a row's sum of exponentials
     int64_t score_stride;
     float scale_log2e, decay;            // |scale| * log2(e)
     uint32_t q_flip;                     // 0x80008000 when scale < 0: every query element changes sign as it is loaded
@@ -664,8 +664,9 @@ struct WeightArgs {
     int32_t max_rows;                    // query rows of a (sequence, KV head): max_q_len * G
     int32_t max_tiles;                   // tiles of products of a sequence
     int32_t whole_waves;                 // both steps in one: waves of a workgroup, else 0
-    int32_t wave_tiles;                  // products kept: tiles of a wave in the first step; else groups of four pages that a workgroup walks, at most kMaxGroups
-    int32_t blocks, block_tokens;        // workgroups of the first step per (sequence, KV head); tokens of one
+    int32_t wave_tiles;                  // products kept: tiles of a wave in the first step; else groups of four pages that a workgroup walks at most, kMaxGroups or fewer
+    int32_t share;                       // products made again: workgroups among which the lengths are dealt out (a multiple of Hkv), 0: wave_tiles groups to each
+    int32_t blocks, block_tokens;        // workgroups of the first step per (sequence, KV head), at most; tokens of one, at most
     int32_t apply_blocks;                // workgroups of the second step per (sequence, KV head), products kept
     int32_t row_blocks;                  // workgroups that join the rows' statistics, products made again
     Division per_group;                  // by G

@@ -435,6 +435,32 @@ struct Stream {
         }
     }
 };
+// Which of a sequence's tokens a workgroup takes: a.wave_tiles groups of pages from group c of sequence b on; or, where a lane can hold every
+// sequence's length (a.share), the fewest with which all workgroups run at once (or in as many turns as the bound on the lengths needs): they are
+// as even as if all lengths were the bound's.  8 sequences of 5 k - 8 k, 256 rows, 8 KV heads: 13 groups each, not 16.
+struct Share {
+    int b, g, c, groups;   // b < 0: none
+};
+SD_DEV int lane_groups(const WeightArgs &a, int lane) { return lane < a.B ? (max(0, min(a.context_lens[lane], a.max_context_len)) + kGroupTokens - 1) / kGroupTokens : 0; }
+SD_DEV int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+SD_DEV int share_groups(const WeightArgs &a, int mine)
+{
+    if (a.share == 0) return a.wave_tiles;
+    const int per_head = a.share / a.Hkv;
+    int w = max(1, (wave_total(mine) + per_head - 1) / per_head);
+    while (w < a.wave_tiles && wave_total((mine + w - 1) / w) > per_head) ++w;   // (wave-uniform)
+    return min(w, a.wave_tiles);
+}
+SD_DEV Share share_of(const WeightArgs &a, int lane)
+{
+    const int g = blockIdx.x % a.Hkv, at = blockIdx.x / a.Hkv;
+    if (a.share == 0) return Share{at / a.blocks, g, at % a.blocks, a.wave_tiles};
+    const int mine = lane_groups(a, lane), w = share_groups(a, mine), parts = (mine + w - 1) / w, upto = wave_scan(parts);
+    const int b = __builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= at));
+    if (b >= 64) return Share{-1, 0, 0, 0};
+    return Share{b, g, at - __builtin_amdgcn_readlane(upto - parts, b), w};
+}
+
 template <int STEPS>
 SD_DEV f32x4 products(const u32x4 (&k)[STEPS], const u32x4 (&q)[STEPS])
 {
@@ -444,23 +470,25 @@ SD_DEV f32x4 products(const u32x4 (&k)[STEPS], const u32x4 (&q)[STEPS])
     return x;
 }
 
-// First step: every row's statistics over the workgroup's tokens.
+// First step: every row's statistics over the workgroup's tokens.  What a row's exponents are taken relative to follows its maximum only
+// once a product is kSlack (a factor of 2^16) above it: the sum of 2^31 such weights is far inside fp32, and a floating sum does not lose by its scale.
+constexpr float kSlack = 16.f;
 template <class K>
 __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightArgs a)
 {
     constexpr int S = K::kDim / 32;
     __shared__ __attribute__((aligned(16))) char s_pages[2 * kGroupPages * K::kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
-    const int g = blockIdx.x % a.Hkv, c = blockIdx.x / a.Hkv % a.blocks, b = blockIdx.x / a.Hkv / a.blocks;
+    const Share share = share_of(a, lane);
+    if (share.b < 0) return;   // workgroup-uniform, as all that follow
+    const int b = share.b, g = share.g, c = share.c;
     const Sequence s = sequence_of(a, b);
-    const int rows = s.n * a.G, page0 = c * a.wave_tiles * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
-    if (page0 > last || rows == 0) return;   // workgroup-uniform (L == 0: last is -1)
-    const Stream<K> stream(a, b, g, page0, last, min(a.wave_tiles, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
+    const int rows = s.n * a.G, page0 = c * share.groups * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
+    if (page0 > last || rows == 0) return;   // (L == 0: last is -1)
+    const Stream<K> stream(a, b, g, page0, last, min(share.groups, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
     float2 *stats = a.stats + (((int64_t)b * a.Hkv + g) * a.blocks + c) * a.max_rows;
     for (int r0 = 0; r0 < rows; r0 += waves * kRowsOfWave) {
         const int first = r0 + wave * kRowsOfWave;   // the wave's first row
-        if (r0) __syncthreads();   // the last group's readers
-        stream.issue(0);
         u32x4 q[kRowTiles][S];
         Stat stat[kRowTiles];
 #pragma unroll
@@ -468,6 +496,8 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
             load_q<K>(q[i], a, s, g, first + i * kMaxGroup + n, rows, lane);
             stat[i] = Stat{-INFINITY, 0.f};
         }
+        if (r0) __syncthreads();   // the last group's readers
+        stream.issue(0);
         for (int group = 0; group < stream.groups; ++group) {
             stream.next(group);
             const int t0 = (page0 + group * kGroupPages) * kPage;
@@ -481,7 +511,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
                     for (int i = 0; i < kRowTiles; ++i) {
                         const int end = masked ? row_end(a, s, first + i * kMaxGroup + n, rows) - t0 - half * kPage - 4 * (lane >> 4) : 0;
                         f32x4 x[kAtOnce];
-                        float m = stat[i].m, by[kAtOnce];   // by: what is left to multiply with
+                        float m = -INFINITY, by[kAtOnce];   // by: what is left to multiply with
 #pragma unroll
                         for (int p = 0; p < kAtOnce; ++p) {
                             x[p] = products(k[p], q[i]);
@@ -491,16 +521,19 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
                                 for (int e = 0; e < 4; ++e) x[p][e] = 16 * p + e < end ? x[p][e] * scale[p] : -INFINITY;
                             m = max_of(m, by[p] * max_of(max_of(x[p][0], x[p][1]), x[p][2], x[p][3]));
                         }
-                        const float ref = reference_of(m);
-                        float l = stat[i].l * shrink_of(stat[i].m, m);
+                        if (__builtin_amdgcn_ballot_w64(m > stat[i].m + kSlack)) {   // wave-uniform
+                            const Stat old = stat[i];
+                            stat[i].m = fmaxf(old.m, m);
+                            stat[i].l = old.l * shrink_of(old.m, stat[i].m);
+                        }
+                        const float ref = reference_of(stat[i].m);
 #pragma unroll
                         for (int p = 0; p < kAtOnce; ++p)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], by[p], -ref));
-                                l += !masked || 16 * p + e < end ? w : 0.f;
+                                stat[i].l += !masked || 16 * p + e < end ? w : 0.f;
                             }
-                        stat[i] = Stat{m, l};
                     }
                 }
             };
@@ -526,7 +559,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(WeightArgs a)
     __shared__ Stat s_stat[4][64];
     const Sequence s = sequence_of(a, (int)(unit / a.Hkv));
     const bool there = r < s.n * a.G;
-    const int blocks = (s.L + a.block_tokens - 1) / a.block_tokens;
+    const int lane = threadIdx.x & 63, tokens = share_groups(a, a.share ? lane_groups(a, lane) : 0) * kGroupTokens, blocks = (s.L + tokens - 1) / tokens;
     Stat sum = {-INFINITY, 0.f};
     if (there) {
         const float2 *v = a.stats + unit * a.blocks * a.max_rows + r;
@@ -544,11 +577,23 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(WeightArgs a)
     if (slice == 0 && there) {
 #pragma unroll
         for (int i = 1; i < 4; ++i) sum = joined(sum, s_stat[i][threadIdx.x]);
-        a.rows[unit * a.max_rows + r] = float2{sum.m, 1.f / sum.l};
+        a.rows[unit * a.max_rows + r] = sum.m + log2f(sum.l);
     }
 }
 
-// Second step: the products once more, and the weights' sums over the rows; grid as in the first.
+// x[p] summed over the four quarters of the wave, each for its own p: lane n + 16 p gets the sum of x[p] over lanes n, n + 16, n + 32, n + 48.
+SD_DEV float over_quarters(const float (&x)[4])
+{
+    const auto bits = [](float f) { return __builtin_bit_cast(unsigned, f); };
+    const auto sum = [](auto y) { return __builtin_bit_cast(float, (unsigned)y[0]) + __builtin_bit_cast(float, (unsigned)y[1]); };
+    const float u = sum(__builtin_amdgcn_permlane32_swap(bits(x[0]), bits(x[2]), false, false));   // halves: x[0], x[2]
+    const float v = sum(__builtin_amdgcn_permlane32_swap(bits(x[1]), bits(x[3]), false, false));   // x[1], x[3]
+    return sum(__builtin_amdgcn_permlane16_swap(bits(u), bits(v), false, false));
+}
+
+// Second step: the products once more, rows by tokens, so that a lane's sum runs over four rows of every tile and only the four quarters of the wave are
+// left to add; and the weights' sums over the rows.  Grid as in the first.  A row's statistics are one number, log2 of its sum of exponentials: a
+// maximum and a reciprocal take twice the registers, which spill (126 us against 88), but leave weights 1e-7 off on average, not 3e-7.
 template <class K>
 __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightArgs a)
 {
@@ -556,56 +601,55 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
     __shared__ __attribute__((aligned(16))) char s_pages[2 * kGroupPages * K::kBytes];
     extern __shared__ float s_sum[];   // [waves][a.block_tokens]: a wave's sums over its rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
-    const int g = blockIdx.x % a.Hkv, c = blockIdx.x / a.Hkv % a.blocks, b = blockIdx.x / a.Hkv / a.blocks;
+    const Share share = share_of(a, lane);
+    if (share.b < 0) return;   // workgroup-uniform, as the next
+    const int b = share.b, g = share.g, c = share.c;
     const Sequence s = sequence_of(a, b);
-    const int rows = s.n * a.G, page0 = c * a.wave_tiles * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
-    if (page0 > last) return;   // workgroup-uniform
+    const int rows = s.n * a.G, page0 = c * share.groups * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
+    if (page0 > last) return;
     const int64_t unit = (int64_t)b * a.Hkv + g;
-    const Stream<K> stream(a, b, g, page0, last, min(a.wave_tiles, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
+    const Stream<K> stream(a, b, g, page0, last, min(share.groups, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
     for (int r0 = 0; r0 < rows; r0 += waves * kRowsOfWave) {
         const int first = r0 + wave * kRowsOfWave;
-        if (r0) __syncthreads();   // the last group's readers
-        stream.issue(0);
         u32x4 q[kRowTiles][S];
-        float2 row[kRowTiles];
+        float row[kRowTiles][4];   // of rows 4 (lane / 16) .. of each tile
 #pragma unroll
         for (int i = 0; i < kRowTiles; ++i) {
-            const int r = first + i * kMaxGroup + n;
-            load_q<K>(q[i], a, s, g, r, rows, lane);
-            row[i] = r < rows ? a.rows[unit * a.max_rows + r] : float2{0.f, 0.f};
+            load_q<K>(q[i], a, s, g, first + i * kMaxGroup + n, rows, lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = first + i * kMaxGroup + 4 * (lane >> 4) + e;
+                row[i][e] = r < rows ? a.rows[unit * a.max_rows + r] : 0.f;
+            }
         }
+        if (r0) __syncthreads();   // the last group's readers
+        stream.issue(0);
         for (int group = 0; group < stream.groups; ++group) {
             stream.next(group);
             const int t0 = (page0 + group * kGroupPages) * kPage;
-            float mine = 0.f;   // over the tiles' rows: the 16 lanes of a group hold the same tokens; lane n keeps token n % 4 of page n / 4
+            float sum[kGroupPages] = {};   // of token n of each page over the lane's rows
             auto tiles = [&](auto masked) {
 #pragma unroll
                 for (int half = 0; half < kGroupPages; half += kAtOnce) {
                     u32x4 k[kAtOnce][S];
                     float scale[kAtOnce];
                     stream.fetch(group, half, k, scale);
-                    f32x4 sum[kAtOnce];
 #pragma unroll
                     for (int i = 0; i < kRowTiles; ++i) {
-                        const int end = masked ? row_end(a, s, first + i * kMaxGroup + n, rows) - t0 - half * kPage - 4 * (lane >> 4) : 0;
+                        int end[4];
+                        if (masked)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) end[e] = row_end(a, s, first + i * kMaxGroup + 4 * (lane >> 4) + e, rows) - t0 - half * kPage - n;
 #pragma unroll
                         for (int p = 0; p < kAtOnce; ++p) {
-                            const f32x4 x = products(k[p], q[i]);
+                            const f32x4 x = products(q[i], k[p]);   // rows by tokens
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale[p], -row[i].x));
-                                const float v = __builtin_fmaf(w, row[i].y, i ? sum[p][e] : 0.f);
-                                sum[p][e] = !masked || 16 * p + e < end ? v : i ? sum[p][e] : 0.f;
+                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale[p], -row[i][e]));
+                                sum[half + p] += !masked || 16 * p < end[e] ? w : 0.f;
                             }
                         }
                     }
-#pragma unroll
-                    for (int p = 0; p < kAtOnce; ++p)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float v = over_rows<16>(sum[p][e]);
-                            mine = n == 4 * (half + p) + e ? v : mine;
-                        }
                 }
             };
             if (first < rows) {   // wave-uniform
@@ -613,7 +657,8 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
                 if (first + kRowsOfWave <= rows && t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});
                 else tiles(std::true_type{});
             }
-            float &kept = s_sum[wave * a.block_tokens + group * kGroupTokens + 16 * (n / 4) + 4 * (lane >> 4) + n % 4];
+            float &kept = s_sum[wave * a.block_tokens + group * kGroupTokens + lane];
+            const float mine = over_quarters(sum);
             kept = r0 ? kept + mine : mine;
         }
     }
@@ -632,7 +677,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
 template <class K>
 static void launch_streamed(const WeightArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((int64_t)a.B * a.blocks * a.Hkv)), block(row_waves(a.max_rows) * 64);
+    const dim3 grid((unsigned)(a.share ? a.share : (int64_t)a.B * a.blocks * a.Hkv)), block(row_waves(a.max_rows) * 64);
     hipLaunchKernelGGL(weight_stats_kernel<K>, grid, block, 0, stream, a);
     if (a.row_blocks) hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)((int64_t)a.B * a.Hkv * a.row_blocks)), dim3(256), 0, stream, a);
     hipLaunchKernelGGL(weight_apply_kernel<K>, grid, block, block.x / 64 * a.block_tokens * 4, stream, a);

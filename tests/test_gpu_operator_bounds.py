@@ -90,3 +90,39 @@ def test_the_largest_budget(sd):
     sd.kv_evict(shape_of(sd, 1, 4, hkv, d, 2 * blocks, blocks, L), budget, 4, 20, torch.rand(1, hkv, L, device="cuda"), L, *pools, None, None, table, lens, new, kept, new_lens)
     assert torch.equal(kept[:L], torch.arange(L, dtype=torch.int32, device="cuda")) and int(kept[L:].max()) == int(kept[L:].min()) == -1
     assert int(new_lens) == L and torch.equal(pools[0][blocks:].view(-1, d)[:L], old.view(-1, d)[:L])
+
+
+@pytest.mark.parametrize("batch", [1, 2, 63, 64, 65, 130])
+@pytest.mark.parametrize("bound", [700, 20000])
+def test_windows_of_as_many_sequences_as_a_wave_holds_and_more(sd, batch, bound):
+    """Up to 64 sequences are dealt out by their lengths, more by the bound; lengths of zero, below the window and far below the bound."""
+    import torch
+    heads, kv_heads, d, most, longest = 8, 2, 64, 7, 700
+    gen = torch.Generator().manual_seed(batch)
+    lens = [int(x) for x in torch.randint(0, longest + 1, (batch,), generator=gen)]
+    lens[0], lens[-1] = longest, 3 if batch > 1 else longest
+    n = [int(x) for x in torch.randint(0, most + 1, (batch,), generator=gen)]
+    starts = [sum(n[:i]) for i in range(batch + 1)]
+    blocks = (bound + 15) // 16
+    pool = torch.randn(batch * 44, kv_heads, 16, d, generator=gen).bfloat16().cuda()
+    table = torch.full((batch, blocks), -1, dtype=torch.int32)
+    table[:, :44] = torch.randperm(batch * 44, generator=gen).view(batch, 44)
+    shape = shape_of(sd, batch, heads, kv_heads, d, batch * 44, blocks, bound)
+    q = queries(max(starts[-1], 1), heads, d, 8)
+    ws = sd.paged_weight_workspace_bytes(shape, most)
+    work = torch.empty(ws, dtype=torch.uint8, device="cuda").fill_(255)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    out = torch.full((batch, kv_heads, bound), -1.0, device="cuda")
+    sd.paged_weight_accumulate(shape, q, dev(starts), starts[-1], most, pool, None, table.cuda(), dev(lens), d ** -0.5, 1.0, 0, None, out, bound, work, ws)
+    for b, L in enumerate(lens):
+        assert bool((out[b, :, L:] == -1).all())
+        k = pool[table[b, :44].long().cuda()].double().transpose(1, 2).reshape(-1, kv_heads, d)[:L]
+        for g in range(kv_heads):
+            want, tol = torch.zeros(L, dtype=torch.float64, device="cuda"), torch.full((L,), 1e-37, dtype=torch.float64, device="cuda")
+            for i in range(n[b]):
+                end = L - n[b] + i + 1
+                if end > 0:
+                    p, t = weights_of(q[starts[b] + i, 4 * g:4 * g + 4].double(), k[:end, g].contiguous(), d ** -0.5)
+                    want[:end] += p
+                    tol[:end] += t
+            assert bool(((out[b, g, :L].double() - want).abs() <= tol).all()), (b, g)
