@@ -2,16 +2,20 @@
 //
 //   s'[b][g][t] = decay s[b][g][t] + sum_rows softmax_t(scale <q_row, K_t>)      rows: the query rows of sequence b, heads of KV head g
 //
-// A weight needs its row's maximum and sum over all tokens, so there are two steps: one over K that makes the products and
-// leaves (max, sum) of every stretch of tokens for each row, and one over the tokens that turns products into weights.
-// The products of one tile of 16 query rows (a decode step: the heads of a KV head) are kept in fp32 between the two,
-// rows * 4 bytes a token, a small part of K's 64 to 256; with more rows (the last tokens of a prompt) K is read and multiplied again.
+// A weight needs its row's maximum and sum over all tokens, so K is walked, each row's statistics are joined, and the products become weights.
 //
 //   S[token][row] = K_page[token][d] . Q^T[d][row]     mfma 16x16x32 bf16, a page of 16 tokens at a time
 //
-// A lane holds four tokens (4 (lane / 16) ..) of row lane % 16.  K goes from memory straight into operand layout: lane n + 16 c
-// reads 16 bytes of token n; which d these are differs between pools, and Q is read in the same order.
-// Weights, sums and scores are fp32 throughout.
+// Up to 16 rows (a decode step: the heads of a KV head) fit one tile, and the products are kept, so K is read once.  Either one workgroup takes a whole
+// (sequence, KV head) and keeps them in its registers (weight_whole_kernel), or they go through memory in fp32, rows * 4 bytes a token beside K's
+// 64 to 256, between two launches (weight_products_kernel, weight_apply_kept_kernel).  Bound by reading K: 256 of 1 k - 8 k, bf16, 7 heads a group:
+// 61 us, 4.4 TB/s of the 6.7 that a plain walk reads, for the longest of a compute unit's sequences ends last; 2048 of 0.5 k - 4 k, fp8: 129 us, 4.8 TB/s.
+// With more rows (the last tokens of a prompt) the products would be more bytes than K: they are made twice, by weight_stats_kernel and
+// weight_apply_kernel, rows stay in registers and K streams past.  Bound by the exponentials and what surrounds them: 8 sequences of 5 k - 8 k,
+// 8 KV heads, 256 rows 41 + 5 + 39 us, 650 and 690 TFLOP/s in the passes; vector units 66 % busy, matrix units 33 %, both at once 12 %.
+//
+// Where products are kept a lane holds four tokens (4 (lane / 16) ..) of row lane % 16.  Which d an operand's 16 bytes are differs between
+// pools, and Q is read in the same order.  Weights, sums and scores are fp32 throughout.
 #include <type_traits>
 
 #include "attn_tile.h"
