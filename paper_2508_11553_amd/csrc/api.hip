@@ -773,7 +773,7 @@ void gradient_blocks(const sd_qk_norm *n, int32_t T, int *q_blocks, int *k_block
 struct WeightPlan {
     int pack;                     // pages to a tile of products that the workspace keeps between the steps; 0: more rows than a tile has, none are kept
     int whole_waves;              // waves of the one kernel that does both steps, else 0
-    int64_t rows, wave_tiles, share, blocks, block_tokens, tiles, apply_blocks, row_blocks, grid;
+    int64_t rows, rounds, wave_tiles, share, blocks, block_tokens, tiles, apply_blocks, row_blocks, grid;
     size_t stats_off, rows_off, total;
 };
 WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
@@ -799,6 +799,7 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
         if (w.whole_waves * per_wave < tokens) w.whole_waves = 0;
     }
     w.share = 0;
+    w.rounds = 1;
     if (w.pack) {
         // A wave's pages: two while that makes no more than 2500 waves, else four (32 units of 4096 14.7 : 13.9, 64 of 1200 12.2 : 12.6); and
         // no more than 128 workgroups to a sequence, whose statistics every workgroup of the second step reads, but at most 64 pages, whose ids its lanes hold.
@@ -809,15 +810,16 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
         // many : these : twice.  256 rows, 8 sequences of 5 k - 8 k, 8 KV heads 84 : 85 : 91, two of 1 k - 4 k 27 : 29 : 39; 16 of 1 k - 4 k: 32 rows 49 : 42 : 51, fp8
         // 45 : 32 : 30, 64 rows 50 : 43 : 52, 128 rows 53 : 53 : 60, head_dim 64 39 : 36 : 40).  That is what the bound asks for; where a wave's lanes hold the
         // lengths, the device deals out as many workgroups by those (16 sequences of 1 k - 8 k, fp8, 256 rows: 86 us by the bound, 63).
-        const int64_t groups = parts(tokens, 4 * sd::kPage), heads = s->num_kv_heads, at_once = kMaxRangeWorkgroups / 2 * std::min(4, 16 / sd::row_waves(w.rows));
-        const int64_t slots = std::max(heads, at_once / heads * heads), all = slots * std::max<int64_t>(1, parts(units * parts(groups, sd::kMaxGroups), slots));
-        w.wave_tiles = std::max<int64_t>(1, parts(units * groups, all));
-        while (units * parts(groups, w.wave_tiles) > all) ++w.wave_tiles;
+        w.rounds = parts(w.rows, sd::row_waves(w.rows) * sd::kRowsOfWave);
+        const int64_t groups = parts(tokens, 4 * sd::kPage), heads = s->num_kv_heads * w.rounds, at_once = kMaxRangeWorkgroups / 2 * std::min(4, 16 / sd::row_waves(w.rows));
+        const int64_t slots = std::max(heads, at_once / heads * heads), all = slots * std::max<int64_t>(1, parts(s->batch * heads * parts(groups, sd::kMaxGroups), slots));
+        w.wave_tiles = std::max<int64_t>(1, parts(s->batch * heads * groups, all));
+        while (s->batch * heads * parts(groups, w.wave_tiles) > all) ++w.wave_tiles;
         if (s->batch <= 64 && all <= 0x7fffffff) w.share = all;
     }
     w.block_tokens = sd::kPage * w.wave_tiles * (w.pack ? sd::kWaves * w.pack : 4);
     w.blocks = parts(tokens, w.share ? 4 * sd::kPage : w.block_tokens);
-    w.grid = w.share ? w.share : units * w.blocks;
+    w.grid = w.share ? w.share : units * w.blocks * w.rounds;
     w.tiles = w.pack ? parts(tokens, w.pack * sd::kPage) : 0;
     w.apply_blocks = parts(tokens, 1024);
     w.row_blocks = parts(w.rows, 64);
@@ -963,8 +965,10 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
     a.scores_out = scores_out;
     a.products = reinterpret_cast<float *>(ws);
     a.stats = reinterpret_cast<float2 *>(ws + w.stats_off);
+    a.parts = reinterpret_cast<float *>(ws + w.stats_off);
     a.rows = reinterpret_cast<float *>(ws + w.rows_off);
     a.score_stride = score_stride;
+    a.part_stride = ((int64_t)shape->max_context_len + 3) & ~(int64_t)3;
     a.scale_log2e = (scale < 0 ? -scale : scale) * 1.4426950408889634f;
     a.q_flip = scale < 0 ? 0x80008000u : 0u;
     a.decay = decay;
@@ -981,6 +985,7 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
     a.max_tiles = (int32_t)w.tiles;
     a.whole_waves = w.whole_waves;
     a.wave_tiles = (int32_t)w.wave_tiles;
+    a.rounds = (int32_t)w.rounds;
     a.share = (int32_t)w.share;
     a.blocks = (int32_t)w.blocks;
     a.block_tokens = (int32_t)w.block_tokens;

@@ -637,7 +637,7 @@ struct NormGradArgs {
 // Attention weights into running scores (weight_scores.hip).
 constexpr int kMaxGroups = 16;    // groups of four pages that a workgroup walks where the products are made twice
 constexpr int kRowsOfWave = 32, kRowWaves = 8;   // rows that a wave holds there, waves of a workgroup at most
-// As many waves as share the rows alike: 800 rows are four rounds of seven waves (98 us, three of eight and one of one 100).
+// As many waves as share the rows alike: 800 rows are four workgroups of seven waves, not three of eight and one of one.
 constexpr int row_waves(int64_t rows)
 {
     const int64_t shares = rows <= kRowsOfWave ? 1 : (rows + kRowsOfWave - 1) / kRowsOfWave, rounds = (shares + kRowWaves - 1) / kRowWaves;
@@ -656,8 +656,9 @@ struct WeightArgs {
     float *scores_out;
     float *products;                     // [B][Hkv][max_tiles][64 lanes][4]: a decode step's, log2 domain
     float2 *stats;                       // (max, sum) of a row over a stretch of tokens.  Products kept: [B][Hkv][blocks][16 / pack], else [B][Hkv][blocks][max_rows]
+    float *parts;                        // several rounds: [rounds][B][Hkv][part_stride], the sums over a round's rows, where the statistics were
     float *rows;                         // [B][Hkv][max_rows]: log2 of a row's sum of exponentials
-    int64_t score_stride;
+    int64_t score_stride, part_stride;
     float scale_log2e, decay;            // |scale| * log2(e)
     uint32_t q_flip;                     // 0x80008000 when scale < 0: every query element changes sign as it is loaded
     int32_t B, Hq, Hkv, G, max_blocks, max_context_len, total_q, max_q_len, new_tokens;
@@ -665,7 +666,8 @@ struct WeightArgs {
     int32_t max_tiles;                   // tiles of products of a sequence
     int32_t whole_waves;                 // both steps in one: waves of a workgroup, else 0
     int32_t wave_tiles;                  // products kept: tiles of a wave in the first step; else groups of four pages that a workgroup walks at most, kMaxGroups or fewer
-    int32_t share;                       // products made again: workgroups among which the lengths are dealt out (a multiple of Hkv), 0: wave_tiles groups to each
+    int32_t rounds;                      // products made again: workgroups that share the rows of a (sequence, KV head)
+    int32_t share;                       // and those among which the lengths are dealt out (a multiple of Hkv * rounds), 0: wave_tiles groups to each
     int32_t blocks, block_tokens;        // workgroups of the first step per (sequence, KV head), at most; tokens of one, at most
     int32_t apply_blocks;                // workgroups of the second step per (sequence, KV head), products kept
     int32_t row_blocks;                  // workgroups that join the rows' statistics, products made again

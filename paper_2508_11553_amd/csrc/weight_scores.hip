@@ -393,9 +393,10 @@ __global__ __launch_bounds__(1024) void weight_whole_kernel(WeightArgs a)
     }
 }
 
-// More rows than a tile: they stay, kRowTiles tiles of them in each wave's registers, and K streams past.  A workgroup walks a.wave_tiles groups of
-// kGroupPages pages of one (sequence, KV head), once for every kRowTiles * 16 * waves rows; its waves bring a group into LDS, a page
-// each, and all read it as operands, kAtOnce pages at a time, while the next one comes.
+// More rows than a tile: they stay, kRowTiles tiles of them in each wave's registers, and K streams past.  A workgroup walks up to a.wave_tiles groups of
+// kGroupPages pages of one (sequence, KV head) for kRowTiles * 16 * waves rows; its waves bring a group into LDS, a page each, and all read it
+// as operands, kAtOnce pages at a time, while the next one comes.  Where there are more rows, other workgroups take them: walking K again in
+// the same one for each round of rows is a start-up each (us: 816 rows, one sequence of 37 k, 2 KV heads 88 : 65; 4096, one of 8 k, 8 KV heads 283 : 180).
 constexpr int kGroupPages = 4, kGroupTokens = kGroupPages * kPage, kAtOnce = 2;
 constexpr int kRowTiles = kRowsOfWave / kMaxGroup;
 template <class K>
@@ -443,26 +444,26 @@ struct Stream {
 // sequence's length (a.share), the fewest with which all workgroups run at once (or in as many turns as the bound on the lengths needs): they are
 // as even as if all lengths were the bound's.  8 sequences of 5 k - 8 k, 256 rows, 8 KV heads: 13 groups each, not 16.
 struct Share {
-    int b, g, c, groups;   // b < 0: none
+    int b, c, groups;   // b < 0: none
 };
 SD_DEV int lane_groups(const WeightArgs &a, int lane) { return lane < a.B ? (max(0, min(a.context_lens[lane], a.max_context_len)) + kGroupTokens - 1) / kGroupTokens : 0; }
 SD_DEV int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 SD_DEV int share_groups(const WeightArgs &a, int mine)
 {
     if (a.share == 0) return a.wave_tiles;
-    const int per_head = a.share / a.Hkv;
+    const int per_head = a.share / (a.Hkv * a.rounds);
     int w = max(1, (wave_total(mine) + per_head - 1) / per_head);
     while (w < a.wave_tiles && wave_total((mine + w - 1) / w) > per_head) ++w;   // (wave-uniform)
     return min(w, a.wave_tiles);
 }
 SD_DEV Share share_of(const WeightArgs &a, int lane)
 {
-    const int g = blockIdx.x % a.Hkv, at = blockIdx.x / a.Hkv;
-    if (a.share == 0) return Share{at / a.blocks, g, at % a.blocks, a.wave_tiles};
+    const int at = blockIdx.x / (a.Hkv * a.rounds);
+    if (a.share == 0) return Share{at / a.blocks, at % a.blocks, a.wave_tiles};
     const int mine = lane_groups(a, lane), w = share_groups(a, mine), parts = (mine + w - 1) / w, upto = wave_scan(parts);
     const int b = __builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= at));
-    if (b >= 64) return Share{-1, 0, 0, 0};
-    return Share{b, g, at - __builtin_amdgcn_readlane(upto - parts, b), w};
+    if (b >= 64) return Share{-1, 0, 0};
+    return Share{b, at - __builtin_amdgcn_readlane(upto - parts, b), w};
 }
 
 template <int STEPS>
@@ -485,73 +486,70 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
     const Share share = share_of(a, lane);
     if (share.b < 0) return;   // workgroup-uniform, as all that follow
-    const int b = share.b, g = share.g, c = share.c;
+    const int b = share.b, c = share.c, g = blockIdx.x % a.Hkv;
     const Sequence s = sequence_of(a, b);
     const int rows = s.n * a.G, page0 = c * share.groups * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
-    if (page0 > last || rows == 0) return;   // (L == 0: last is -1)
+    const int first = (blockIdx.x / a.Hkv % a.rounds * waves + wave) * kRowsOfWave;   // the wave's first row
+    if (page0 > last || first - wave * kRowsOfWave >= rows) return;   // (L == 0: last is -1)
     const Stream<K> stream(a, b, g, page0, last, min(share.groups, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
     float2 *stats = a.stats + (((int64_t)b * a.Hkv + g) * a.blocks + c) * a.max_rows;
-    for (int r0 = 0; r0 < rows; r0 += waves * kRowsOfWave) {
-        const int first = r0 + wave * kRowsOfWave;   // the wave's first row
-        u32x4 q[kRowTiles][S];
-        Stat stat[kRowTiles];
+    u32x4 q[kRowTiles][S];
+    Stat stat[kRowTiles];
 #pragma unroll
-        for (int i = 0; i < kRowTiles; ++i) {
-            load_q<K>(q[i], a, s, g, first + i * kMaxGroup + n, rows, lane);
-            stat[i] = Stat{-INFINITY, 0.f};
-        }
-        if (r0) __syncthreads();   // the last group's readers
-        stream.issue(0);
-        for (int group = 0; group < stream.groups; ++group) {
-            stream.next(group);
-            const int t0 = (page0 + group * kGroupPages) * kPage;
-            auto tiles = [&](auto masked) {
+    for (int i = 0; i < kRowTiles; ++i) {
+        load_q<K>(q[i], a, s, g, first + i * kMaxGroup + n, rows, lane);
+        stat[i] = Stat{-INFINITY, 0.f};
+    }
+    stream.issue(0);
+    for (int group = 0; group < stream.groups; ++group) {
+        stream.next(group);
+        const int t0 = (page0 + group * kGroupPages) * kPage;
+        auto tiles = [&](auto masked) {
 #pragma unroll
-                for (int half = 0; half < kGroupPages; half += kAtOnce) {
-                    u32x4 k[kAtOnce][S];
-                    float scale[kAtOnce];
-                    stream.fetch(group, half, k, scale);
+            for (int half = 0; half < kGroupPages; half += kAtOnce) {
+                u32x4 k[kAtOnce][S];
+                float scale[kAtOnce];
+                stream.fetch(group, half, k, scale);
 #pragma unroll
-                    for (int i = 0; i < kRowTiles; ++i) {
-                        const int end = masked ? row_end(a, s, first + i * kMaxGroup + n, rows) - t0 - half * kPage - 4 * (lane >> 4) : 0;
-                        f32x4 x[kAtOnce];
-                        float m = -INFINITY, by[kAtOnce];   // by: what is left to multiply with
+                for (int i = 0; i < kRowTiles; ++i) {
+                    const int end = masked ? row_end(a, s, first + i * kMaxGroup + n, rows) - t0 - half * kPage - 4 * (lane >> 4) : 0;
+                    f32x4 x[kAtOnce];
+                    float m = -INFINITY, by[kAtOnce];   // by: what is left to multiply with
 #pragma unroll
-                        for (int p = 0; p < kAtOnce; ++p) {
-                            x[p] = products(k[p], q[i]);
-                            by[p] = masked ? 1.f : scale[p];
-                            if (masked)
+                    for (int p = 0; p < kAtOnce; ++p) {
+                        x[p] = products(k[p], q[i]);
+                        by[p] = masked ? 1.f : scale[p];
+                        if (masked)
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) x[p][e] = 16 * p + e < end ? x[p][e] * scale[p] : -INFINITY;
-                            m = max_of(m, by[p] * max_of(max_of(x[p][0], x[p][1]), x[p][2], x[p][3]));
-                        }
-                        if (__builtin_amdgcn_ballot_w64(m > stat[i].m + kSlack)) {   // wave-uniform
-                            const Stat old = stat[i];
-                            stat[i].m = fmaxf(old.m, m);
-                            stat[i].l = old.l * shrink_of(old.m, stat[i].m);
-                        }
-                        const float ref = reference_of(stat[i].m);
-#pragma unroll
-                        for (int p = 0; p < kAtOnce; ++p)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], by[p], -ref));
-                                stat[i].l += !masked || 16 * p + e < end ? w : 0.f;
-                            }
+                            for (int e = 0; e < 4; ++e) x[p][e] = 16 * p + e < end ? x[p][e] * scale[p] : -INFINITY;
+                        m = max_of(m, by[p] * max_of(max_of(x[p][0], x[p][1]), x[p][2], x[p][3]));
                     }
-                }
-            };
-            if (first >= rows) continue;   // wave-uniform: rows that are not there
-            if (t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});   // every row attends all of these tokens
-            else tiles(std::true_type{});
-        }
+                    if (__builtin_amdgcn_ballot_w64(m > stat[i].m + kSlack)) {   // wave-uniform
+                        const Stat old = stat[i];
+                        stat[i].m = fmaxf(old.m, m);
+                        stat[i].l = old.l * shrink_of(old.m, stat[i].m);
+                    }
+                    const float ref = reference_of(stat[i].m);
 #pragma unroll
-        for (int i = 0; i < kRowTiles; ++i) {
-            Stat all = stat[i];
-            for (int off = 16; off < 64; off *= 2) all = joined(all, Stat{__shfl_xor(all.m, off, 64), __shfl_xor(all.l, off, 64)});
-            const int r = first + i * kMaxGroup + n;
-            if (lane < 16 && r < rows) stats[r] = float2{all.m, all.l};
-        }
+                    for (int p = 0; p < kAtOnce; ++p)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], by[p], -ref));
+                            stat[i].l += !masked || 16 * p + e < end ? w : 0.f;
+                        }
+                }
+            }
+        };
+        if (first >= rows) continue;   // wave-uniform: rows that are not there
+        if (t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});   // every row attends all of these tokens
+        else tiles(std::true_type{});
+    }
+#pragma unroll
+    for (int i = 0; i < kRowTiles; ++i) {
+        Stat all = stat[i];
+        for (int off = 16; off < 64; off *= 2) all = joined(all, Stat{__shfl_xor(all.m, off, 64), __shfl_xor(all.l, off, 64)});
+        const int r = first + i * kMaxGroup + n;
+        if (lane < 16 && r < rows) stats[r] = float2{all.m, all.l};
     }
 }
 
@@ -607,14 +605,14 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
     const Share share = share_of(a, lane);
     if (share.b < 0) return;   // workgroup-uniform, as the next
-    const int b = share.b, g = share.g, c = share.c;
+    const int b = share.b, c = share.c, g = blockIdx.x % a.Hkv, round = blockIdx.x / a.Hkv % a.rounds;
     const Sequence s = sequence_of(a, b);
     const int rows = s.n * a.G, page0 = c * share.groups * kGroupPages, last = (s.L + kPage - 1) / kPage - 1, n = lane & 15;
-    if (page0 > last) return;
+    const int first = (round * waves + wave) * kRowsOfWave;
+    if (page0 > last || (round && first - wave * kRowsOfWave >= rows)) return;
     const int64_t unit = (int64_t)b * a.Hkv + g;
     const Stream<K> stream(a, b, g, page0, last, min(share.groups, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
-    for (int r0 = 0; r0 < rows; r0 += waves * kRowsOfWave) {
-        const int first = r0 + wave * kRowsOfWave;
+    if (rows) {
         u32x4 q[kRowTiles][S];
         float row[kRowTiles][4];   // of rows 4 (lane / 16) .. of each tile
 #pragma unroll
@@ -626,7 +624,6 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
                 row[i][e] = r < rows ? a.rows[unit * a.max_rows + r] : 0.f;
             }
         }
-        if (r0) __syncthreads();   // the last group's readers
         stream.issue(0);
         for (int group = 0; group < stream.groups; ++group) {
             stream.next(group);
@@ -661,9 +658,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
                 if (first + kRowsOfWave <= rows && t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});
                 else tiles(std::true_type{});
             }
-            float &kept = s_sum[wave * a.block_tokens + group * kGroupTokens + lane];
-            const float mine = over_quarters(sum);
-            kept = r0 ? kept + mine : mine;
+            s_sum[wave * a.block_tokens + group * kGroupTokens + lane] = over_quarters(sum);
         }
     }
     __syncthreads();
@@ -673,18 +668,39 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
         float all = 0.f;
         if (rows)
             for (int w = 0; w < waves; ++w) all += s_sum[w * a.block_tokens + i];
+        if (a.rounds > 1) {
+            a.parts[((int64_t)round * a.B * a.Hkv + unit) * a.part_stride + t] = all;
+            continue;
+        }
         const int64_t at = unit * a.score_stride + t;
         a.scores_out[at] = all + (a.scores_in && t < s.L - a.new_tokens ? a.decay * a.scores_in[at] : 0.f);
     }
 }
 
+// Where the rows take several rounds: their sums, four tokens to a thread.
+__global__ __launch_bounds__(256) void weight_join_kernel(WeightArgs a)
+{
+    const int64_t unit = blockIdx.x / a.apply_blocks;
+    const int t0 = blockIdx.x % a.apply_blocks * kApplyTokens + 4 * threadIdx.x;
+    const Sequence s = sequence_of(a, (int)(unit / a.Hkv));
+    if (t0 >= s.L) return;
+    f32x4 sum = {0, 0, 0, 0};
+    for (int first = 0, round = 0; first < s.n * a.G; first += row_waves(a.max_rows) * kRowsOfWave, ++round)
+        sum += *reinterpret_cast<const f32x4 *>(a.parts + ((int64_t)round * a.B * a.Hkv + unit) * a.part_stride + t0);
+    const int64_t at = unit * a.score_stride + t0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (t0 + e < s.L) a.scores_out[at + e] = sum[e] + (a.scores_in && t0 + e < s.L - a.new_tokens ? a.decay * a.scores_in[at + e] : 0.f);
+}
+
 template <class K>
 static void launch_streamed(const WeightArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.share ? a.share : (int64_t)a.B * a.blocks * a.Hkv)), block(row_waves(a.max_rows) * 64);
+    const dim3 grid((unsigned)(a.share ? a.share : (int64_t)a.B * a.blocks * a.Hkv * a.rounds)), block(row_waves(a.max_rows) * 64);
     hipLaunchKernelGGL(weight_stats_kernel<K>, grid, block, 0, stream, a);
     if (a.row_blocks) hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)((int64_t)a.B * a.Hkv * a.row_blocks)), dim3(256), 0, stream, a);
     hipLaunchKernelGGL(weight_apply_kernel<K>, grid, block, block.x / 64 * a.block_tokens * 4, stream, a);
+    if (a.rounds > 1) hipLaunchKernelGGL(weight_join_kernel, dim3((unsigned)((int64_t)a.B * a.Hkv * a.apply_blocks)), dim3(256), 0, stream, a);
 }
 
 template <class K, int PACK>

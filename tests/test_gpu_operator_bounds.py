@@ -126,3 +126,46 @@ def test_windows_of_as_many_sequences_as_a_wave_holds_and_more(sd, batch, bound)
                     want[:end] += p
                     tol[:end] += t
             assert bool(((out[b, g, :L].double() - want).abs() <= tol).all()), (b, g)
+
+
+@pytest.mark.parametrize("batch,heads,most,d,kv", [(3, 8, 300, 64, "bf16"), (2, 16, 65, 128, "fp8"), (66, 16, 40, 64, "bf16"), (1, 64, 100, 64, "fp8")])
+def test_rows_of_several_workgroups(sd, batch, heads, most, d, kv):
+    """One KV head, up to 6400 rows: sequences with all of the bound's rows, with one and with none, windows longer than the sequence, scores in place."""
+    import torch
+    gen = torch.Generator().manual_seed(most)
+    lens = [most + 500 - 37 * (b % 13) for b in range(batch)]
+    n = [(most, 1, 0, most // 2, most)[b % 5] for b in range(batch)]
+    lens[-1] = most - 7 if batch > 1 else lens[-1]   # rows of negative positions
+    starts = [sum(n[:i]) for i in range(batch + 1)]
+    bound, per = (max(lens) + 3) // 4 * 4, (max(lens) + 15) // 16
+    tile = torch.randn(batch * per, 1, 16, d, generator=gen)
+    scales = torch.rand(batch * per, 1, generator=gen) * 0.5 + 0.75 if kv == "fp8" else None
+    pool = tile.to(torch.float8_e4m3fn if kv == "fp8" else torch.bfloat16).cuda()
+    values = pool.double() * (scales.cuda().double()[:, :, None, None] if kv == "fp8" else 1.0)
+    table = torch.randperm(batch * per, generator=gen).view(batch, per).int().cuda()
+    shape = shape_of(sd, batch, heads, 1, d, batch * per, per, bound, kv)
+    q = queries(starts[-1], heads, d, 9)
+    scores = torch.rand(batch, 1, bound, device="cuda") * 3
+    before = scores.clone().double()
+    ws = sd.paged_weight_workspace_bytes(shape, most)
+    work = torch.empty(ws, dtype=torch.uint8, device="cuda").fill_(255)
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    sd.paged_weight_accumulate(shape, q, dev(starts), starts[-1], most, pool.view(torch.uint8) if kv == "fp8" else pool, scales.cuda() if kv == "fp8" else None, table, dev(lens),
+                               d ** -0.5, 0.75, 3, scores, scores, bound, work, ws)
+    for b, L in enumerate(lens):
+        k = values[table[b].long(), 0].reshape(-1, d)[:L]
+        want = 0.75 * before[b, 0, :L]
+        want[L - 3:] = 0
+        tol = 8 * U * want + 1e-37
+        pos = torch.arange(L - n[b], L, device="cuda").repeat_interleave(heads)
+        x = d ** -0.5 * (q[starts[b]:starts[b + 1]].double().reshape(-1, d) @ k.T)
+        size = d ** -0.5 * (q[starts[b]:starts[b + 1]].double().abs().reshape(-1, d) @ k.abs().T)
+        seen = torch.arange(L, device="cuda")[None] <= pos[:, None]
+        x, size, seen = x[pos >= 0], size[pos >= 0], seen[pos >= 0]
+        if len(x):
+            p = torch.softmax(x.masked_fill(~seen, float("-inf")), 1)
+            off = 3 * (d + 4) * size.masked_fill(~seen, 0).amax(1, keepdim=True) * U + (64 + x.masked_fill(~seen, 0).abs().amax(1, keepdim=True)) * 2 * U
+            want, tol = want + p.sum(0), tol + (p * off + 1e-37 * seen).sum(0)
+        got = scores[b, 0, :L].double()
+        assert bool(((got - want).abs() <= tol + 80 * U * want).all()), b
+        assert torch.equal(scores[b, 0, L:].double(), before[b, 0, L:])
