@@ -12,7 +12,7 @@
 // 61 us, 4.4 TB/s of the 6.7 that a plain walk reads, for the longest of a compute unit's sequences ends last; 2048 of 0.5 k - 4 k, fp8: 129 us, 4.8 TB/s.
 // With more rows (the last tokens of a prompt) the products would be more bytes than K: they are made twice, by weight_stats_kernel and
 // weight_apply_kernel, rows stay in registers and K streams past.  Bound by the exponentials and what surrounds them: 8 sequences of 5 k - 8 k,
-// 8 KV heads, 256 rows 41 + 5 + 39 us, 650 and 690 TFLOP/s in the passes; vector units 66 % busy, matrix units 33 %, both at once 12 %.
+// 8 KV heads, 256 rows 41 + 5 + 39 us, 650 and 690 TFLOP/s in the passes; vector units 61 - 68 % busy, matrix units 35 %, both at once 13 %.
 //
 // Where products are kept a lane holds four tokens (4 (lane / 16) ..) of row lane % 16.  Which d an operand's 16 bytes are differs between
 // pools, and Q is read in the same order.  Weights, sums and scores are fp32 throughout.
