@@ -984,6 +984,7 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
     a.max_rows = (int32_t)w.rows;
     a.max_tiles = (int32_t)w.tiles;
     a.whole_waves = w.whole_waves;
+    a.long_first = w.whole_waves && units > kMaxRangeWorkgroups / 2 && shape->batch <= 64 * sd::kLaneLengths;   // more than compute units
     a.wave_tiles = (int32_t)w.wave_tiles;
     a.rounds = (int32_t)w.rounds;
     a.share = (int32_t)w.share;

@@ -636,6 +636,7 @@ struct NormGradArgs {
 
 // Attention weights into running scores (weight_scores.hip).
 constexpr int kMaxGroups = 16;    // groups of four pages that a workgroup walks where the products are made twice
+constexpr int kLaneLengths = 4;   // sequences whose lengths a lane holds, where long ones come first
 constexpr int kRowsOfWave = 32, kRowWaves = 8;   // rows that a wave holds there, waves of a workgroup at most
 // As many waves as share the rows alike: 800 rows are four workgroups of seven waves, not three of eight and one of one.
 constexpr int row_waves(int64_t rows)
@@ -665,6 +666,7 @@ struct WeightArgs {
     int32_t max_rows;                    // query rows of a (sequence, KV head): max_q_len * G
     int32_t max_tiles;                   // tiles of products of a sequence
     int32_t whole_waves;                 // both steps in one: waves of a workgroup, else 0
+    int32_t long_first;                  // there: sequences longer than half the bound come first
     int32_t wave_tiles;                  // products kept: tiles of a wave in the first step; else groups of four pages that a workgroup walks at most, kMaxGroups or fewer
     int32_t rounds;                      // products made again: workgroups that share the rows of a (sequence, KV head)
     int32_t share;                       // and those among which the lengths are dealt out (a multiple of Hkv * rounds), 0: wave_tiles groups to each

@@ -9,7 +9,7 @@
 // Up to 16 rows (a decode step: the heads of a KV head) fit one tile, and the products are kept, so K is read once.  Either one workgroup takes a whole
 // (sequence, KV head) and keeps them in its registers (weight_whole_kernel), or they go through memory in fp32, rows * 4 bytes a token beside K's
 // 64 to 256, between two launches (weight_products_kernel, weight_apply_kept_kernel).  Bound by reading K: 256 of 1 k - 8 k, bf16, 7 heads a group:
-// 61 us, 4.4 TB/s of the 6.7 that a plain walk reads, for the longest of a compute unit's sequences ends last; 2048 of 0.5 k - 4 k, fp8: 129 us, 4.8 TB/s.
+// 61 us, 4.4 TB/s of the 6.7 that a plain walk reads, for the longest of a compute unit's sequences ends last; 2048 of 0.5 k - 4 k, fp8: 117 us, 5.3 TB/s.
 // With more rows (the last tokens of a prompt) the products would be more bytes than K: they are made twice, by weight_stats_kernel and
 // weight_apply_kernel, rows stay in registers and K streams past.  Bound by the exponentials and what surrounds them: 8 sequences of 5 k - 8 k,
 // 8 KV heads, 256 rows 41 + 5 + 39 us, 650 and 690 TFLOP/s in the passes; vector units 61 - 68 % busy, matrix units 35 %, both at once 13 %.
@@ -319,6 +319,34 @@ __global__ __launch_bounds__(256) void weight_apply_kept_kernel(WeightArgs a)
     }
 }
 
+// The sequence of a workgroup where those longer than half the bound come first: as workgroups end, the next ones are short (us: 128 sequences of
+// 1 k - 8 k, 4 KV heads 123 : 109; 256 of 0.5 k - 4 k, fp8, 8 KV heads 126 : 117; 200 of one length 164 : 164).
+SD_DEV int long_first(const WeightArgs &a, int at, int lane)
+{
+    int len[kLaneLengths];
+    unsigned long long longs[kLaneLengths];
+    int all_long = 0;
+#pragma unroll
+    for (int j = 0; j < kLaneLengths; ++j) len[j] = 64 * j + lane < a.B ? a.context_lens[64 * j + lane] : 0;
+#pragma unroll
+    for (int j = 0; j < kLaneLengths; ++j) {
+        longs[j] = __builtin_amdgcn_ballot_w64(len[j] > a.max_context_len / 2);
+        all_long += __builtin_popcountll(longs[j]);
+    }
+    const bool is_long = at < all_long;   // wave-uniform: the at-th of the long ones, or of the others
+    if (!is_long) at -= all_long;
+    int b = 0;
+#pragma unroll
+    for (int j = 0; j < kLaneLengths; ++j) {
+        const unsigned long long these = is_long ? longs[j] : ~longs[j];
+        const int rank = __builtin_amdgcn_mbcnt_hi((unsigned)(these >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)these, 0));
+        const unsigned long long it = __builtin_amdgcn_ballot_w64((these >> lane & 1) && rank == at);
+        if (it) b = 64 * j + __builtin_ctzll(it);
+        at -= __builtin_popcountll(these);
+    }
+    return b;
+}
+
 // Both steps in one: a workgroup takes a whole (sequence, KV head) and its products stay in its registers, whole_tiles to a wave.
 template <class K, int PACK>
 __global__ __launch_bounds__(1024) void weight_whole_kernel(WeightArgs a)
@@ -327,7 +355,7 @@ __global__ __launch_bounds__(1024) void weight_whole_kernel(WeightArgs a)
     extern __shared__ __attribute__((aligned(16))) char s_pages[];   // [waves][2][K::kBytes]
     __shared__ Stat s_stat[16][W];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x / 64;
-    const int g = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
+    const int g = blockIdx.x % a.Hkv, b = a.long_first ? long_first(a, blockIdx.x / a.Hkv, lane) : blockIdx.x / a.Hkv;
     const Sequence s = sequence_of(a, b);
     if (s.L == 0) return;
     const int64_t unit = (int64_t)b * a.Hkv + g;

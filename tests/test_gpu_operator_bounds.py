@@ -169,3 +169,30 @@ def test_rows_of_several_workgroups(sd, batch, heads, most, d, kv):
         got = scores[b, 0, :L].double()
         assert bool(((got - want).abs() <= tol + 80 * U * want).all()), b
         assert torch.equal(scores[b, 0, L:].double(), before[b, 0, L:])
+
+
+@pytest.mark.parametrize("batch", [65, 100, 256, 257])
+@pytest.mark.parametrize("bound", [400, 900])
+def test_every_sequence_once_whatever_the_order(sd, batch, bound):
+    """More (sequence, KV head)s than compute units: the longer sequences' workgroups come first, up to 256 sequences."""
+    import torch
+    heads, kv_heads, d, longest = 8, 4, 64, 400
+    gen = torch.Generator().manual_seed(batch)
+    lens = torch.randint(0, longest + 1, (batch,), generator=gen)
+    lens[0], lens[1], lens[-1] = 0, 1, longest
+    per, blocks = 25, (bound + 15) // 16
+    pool = torch.randn(batch * per, kv_heads, 16, d, generator=gen).bfloat16().cuda()
+    table = torch.full((batch, blocks), -1, dtype=torch.int32)
+    table[:, :per] = torch.randperm(batch * per, generator=gen).view(batch, per)
+    q = queries(batch, heads, d, 8)
+    shape = shape_of(sd, batch, heads, kv_heads, d, batch * per, blocks, bound)
+    ws = sd.paged_weight_workspace_bytes(shape, 1)
+    work = torch.empty(ws, dtype=torch.uint8, device="cuda").fill_(255)
+    out = torch.full((batch, kv_heads, bound), -1.0, device="cuda")
+    sd.paged_weight_accumulate(shape, q, None, batch, 1, pool, None, table.cuda(), lens.int().cuda(), d ** -0.5, 1.0, 0, None, out, bound, work, ws)
+    for b, L in enumerate(lens.tolist()):
+        assert bool((out[b, :, L:] == -1).all())
+        k = pool[table[b, :per].long().cuda()].double().transpose(1, 2).reshape(-1, kv_heads, d)[:L]
+        for g in range(kv_heads if L else 0):
+            want, tol = weights_of(q[b, 2 * g:2 * g + 2].double(), k[:, g].contiguous(), d ** -0.5)
+            assert bool(((out[b, g, :L].double() - want).abs() <= tol).all()), (b, g)
