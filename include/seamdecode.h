@@ -444,8 +444,8 @@ int qk_norm_rope_backward(const sd_qk_norm *norm, const void *dq_out, const void
  * sequence b owns the rows q_start[b] .. q_start[b+1]-1, as in
  * paged_prefill_attention: row i of n_b is the query of position L - n_b + i
  * and attends the tokens up to that one; rows of negative positions add
- * nothing, nor do those past max_q_len (which should not exist: the bound is
- * the caller's).  Weights and scores are fp32.
+ * nothing, nor do those past max_q_len (rows i >= max_q_len; the others keep
+ * the positions that n_b gives them).  Weights and scores are fp32.
  *
  *   q            bf16 [total_q][num_q_heads][d]
  *   q_start      i32 [batch + 1] or NULL (then total_q is batch and max_q_len 1); a sequence

@@ -92,6 +92,7 @@ SD_DEV void wait_reads()
 // What a workgroup knows of its sequence.
 struct Sequence {
     int L, first_q, n;   // tokens, first query row, query rows of it
+    int base;            // position of the first one, which the whole range gives it; may be negative
 };
 SD_DEV Sequence sequence_of(const WeightArgs &a, int b)
 {
@@ -99,11 +100,13 @@ SD_DEV Sequence sequence_of(const WeightArgs &a, int b)
     s.L = max(0, min(a.context_lens[b], a.max_context_len));
     s.first_q = b;
     s.n = 1;
+    s.base = s.L - 1;
     if (a.q_start) {
         const int q0 = a.q_start[b], q1 = a.q_start[b + 1];
         const bool inside = q0 >= 0 && q1 <= a.total_q && q1 > q0;   // a range that leaves the rows has none
         s.first_q = inside ? q0 : 0;
         s.n = inside ? min(q1 - q0, a.max_q_len) : 0;
+        s.base = inside ? s.L - (q1 - q0) : s.L;
     }
     return s;
 }
@@ -120,7 +123,7 @@ SD_DEV void load_q(u32x4 (&q)[K::kDim / 32], const WeightArgs &a, const Sequence
 }
 
 // The tokens that row r attends: those before `end`.
-SD_DEV int row_end(const WeightArgs &a, const Sequence &s, int r, int rows) { return r < rows ? min(s.L, s.L - s.n + 1 + (int)a.per_group.of(r)) : 0; }
+SD_DEV int row_end(const WeightArgs &a, const Sequence &s, int r, int rows) { return r < rows ? min(s.L, s.base + 1 + (int)a.per_group.of(r)) : 0; }
 
 struct Stat {
     float m, l;   // maximum (log2 domain) and sum of exp2(x - m)
@@ -569,7 +572,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
             }
         };
         if (first >= rows) continue;   // wave-uniform: rows that are not there
-        if (t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});   // every row attends all of these tokens
+        if (t0 + kGroupTokens <= s.base + 1) tiles(std::false_type{});   // every row attends all of these tokens
         else tiles(std::true_type{});
     }
 #pragma unroll
@@ -683,7 +686,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
             };
             if (first < rows) {   // wave-uniform
                 // every row is there and attends all of these tokens (one that is not there gives 0 * K, which an infinite K makes NaN)
-                if (first + kRowsOfWave <= rows && t0 + kGroupTokens <= s.L - s.n + 1) tiles(std::false_type{});
+                if (first + kRowsOfWave <= rows && t0 + kGroupTokens <= s.base + 1) tiles(std::false_type{});
                 else tiles(std::true_type{});
             }
             s_sum[wave * a.block_tokens + group * kGroupTokens + lane] = over_quarters(sum);
