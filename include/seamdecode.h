@@ -336,7 +336,8 @@ int paged_decode_attention_prefix(const sd_shape *shape, const void *q,
  *   q         bf16 [total_q][num_q_heads][head_dim]  (device)
  *   q_start   i32 [batch + 1] (device), ascending, q_start[batch] <= total_q; a
  *             sequence whose range leaves [0, total_q) is skipped
- *   max_q_len host-known bound on n_b; rows past it in a sequence are not computed
+ *   max_q_len host-known bound on n_b; rows past it in a sequence are not computed, the others keep
+ *             the positions that n_b gives them
  *   out       f32 [total_q][num_q_heads][head_dim]   (device); rows no sequence owns are left as they are
  *   timer     NULL or an sd_timer; the kernel's time is reported as split_ms, merge_ms reads ~0
  */

@@ -45,7 +45,7 @@ struct WaveSequences {
             const int nq = min(next - qs, a.max_q_len);
             L = max(0, min(L, a.max_context_len));
             // rounded up; a.reciprocal = 2^32 / tokens of a workgroup, rounded up: exact below 2^24
-            if (lane < a.B && qs >= 0 && nq > 0 && (int64_t)qs + nq <= a.total_q) {
+            if (lane < a.B && qs >= 0 && nq > 0 && next <= a.total_q) {
                 blocks = (int)__umulhi((unsigned)(nq + a.round_up), a.reciprocal);
                 end = (int)__umulhi((unsigned)(L + a.round_up), a.reciprocal);
             }
@@ -76,7 +76,7 @@ struct WaveLengths {
         int qs = 0, next = 0, stored = 0;
         if (lane < a.B) qs = a.q_start[lane], next = a.q_start[lane + 1], stored = a.context_lens[lane];
         const int n = min(next - qs, a.max_q_len);
-        if (lane < a.B && qs >= 0 && n > 0 && (int64_t)qs + n <= a.total_q) nq = n, L = max(0, min(stored, a.max_context_len));
+        if (lane < a.B && qs >= 0 && n > 0 && next <= a.total_q) nq = n, L = max(0, min(stored, a.max_context_len));
     }
     SD_DEV int count(int tokens, int halves) const { return (int)__umulhi((unsigned)((tokens << halves) + round_up), reciprocal); }   // as above
     SD_DEV int longest() const { return wave_max(nq > 0 ? L : 0); }
@@ -120,12 +120,13 @@ struct PrefillRows {
         b = seq;
         hb = head_block(head, a.G, a.HB);
         qs = a.q_start[b];
-        nq = min(a.q_start[b + 1] - qs, a.max_q_len);
+        const int next = a.q_start[b + 1];
+        nq = min(next - qs, a.max_q_len);
         const int i0 = jb * groups * tpw;
         if (i0 >= nq) return false;
-        if (qs < 0 || (int64_t)qs + nq > a.total_q) return false;  // rows outside q: nothing is read or written
+        if (qs < 0 || next > a.total_q) return false;  // rows outside q: nothing is read or written
         L = max(0, min(a.context_lens[b], a.max_context_len));
-        base = L - nq;
+        base = L - (next - qs);   // rows past max_q_len are not computed, but the others stand where the whole range puts them
         kv_end = max(0, base + min(nq, i0 + groups * tpw));
         iw0 = i0 + group * tpw;
         const int iw1 = min(iw0 + tpw, nq);

@@ -2,7 +2,9 @@
 import numpy as np
 import pytest
 
+from tests.test_gpu_prefill import check as check_rows, gpu, make_bound, ref
 from tests.test_gpu_weight_scores import U, Cache, check, queries, run
+from tests.test_prefill_geometry import PLANS, context_bound, plan as route_of, program, stretch_case  # noqa: F401  (program is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +55,27 @@ def test_weights(sd, lens, rows, most, hq, hkv, d, kv):
     q = queries(int(starts[-1]), hq, d, 2, 1.5)
     got = run(sd, c, hq, q, starts, d ** -0.5, 1.0, 0, None, max_q_len=most)
     check(got, weights_within(c, q.double().cpu().numpy(), starts, most, d ** -0.5), lens)
+
+
+@pytest.mark.parametrize("kv,d,plan", PLANS)
+def test_attention(sd, program, kv, d, plan):
+    """Every kernel of the causal pass, at its own size: what it writes are the rows within the bound, as the whole ranges have them, and no others."""
+    lens, nq, Hq, Hkv = stretch_case(plan, d)
+    bound, most = context_bound(plan[0], d), max(nq)
+    more = list(nq)
+    more[nq.index(most)] += 23   # one is longer than the bound
+    assert route_of(program, lens, more, Hq, Hkv, d, kv, bound, most) == plan
+    wl, q, q_start = make_bound(lens, more, Hq, Hkv, d, kv, bound, seed=900 + d)
+    got, want = gpu(wl, q, q_start, max_q=most), ref(wl, q, q_start)
+    within = np.concatenate([np.arange(n) < most for n in more])
+    assert (~within).sum() == 23
+    assert np.isnan(got[~within]).all()
+    check_rows(got[within], want[within], kv)
+    # a range that leaves the rows has none, though those within the bound lie inside
+    few = nq[-1]
+    outside = q_start.copy()
+    outside[-1] = len(q) + 5
+    got, inner = gpu(wl, q, outside, max_q=few), slice(0, q_start[-2])
+    assert np.isnan(got[q_start[-2]:]).all()
+    within = np.concatenate([np.arange(n) < few for n in more])[inner]
+    check_rows(got[inner][within], want[inner][within], kv)
