@@ -830,7 +830,7 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
         const int64_t most_blocks = parts(tokens, pack ? sd::kPage * sd::kWaves * pack * parts(2, pack) : 4 * sd::kPage);
         w.stats_off = pack ? up((size_t)units * parts(tokens, pack * sd::kPage) * 1024) : 0;
         w.rows_off = w.stats_off + up((size_t)units * most_blocks * (pack ? sd::kMaxGroup / pack : rows) * 8);
-        return w.rows_off + (pack ? 0 : up((size_t)units * rows * 4));
+        return w.rows_off + (pack ? 0 : up((size_t)units * rows * 8));
     };
     const int64_t group = s->num_q_heads / s->num_kv_heads;
     const size_t fewer = layout(std::min(w.rows, sd::kMaxGroup / group * group));
@@ -966,7 +966,7 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
     a.products = reinterpret_cast<float *>(ws);
     a.stats = reinterpret_cast<float2 *>(ws + w.stats_off);
     a.parts = reinterpret_cast<float *>(ws + w.stats_off);
-    a.rows = reinterpret_cast<float *>(ws + w.rows_off);
+    a.rows = reinterpret_cast<float2 *>(ws + w.rows_off);
     a.score_stride = score_stride;
     a.part_stride = ((int64_t)shape->max_context_len + 3) & ~(int64_t)3;
     a.scale_log2e = (scale < 0 ? -scale : scale) * 1.4426950408889634f;

@@ -658,7 +658,7 @@ struct WeightArgs {
     float *products;                     // [B][Hkv][max_tiles][64 lanes][4]: a decode step's, log2 domain
     float2 *stats;                       // (max, sum) of a row over a stretch of tokens.  Products kept: [B][Hkv][blocks][16 / pack], else [B][Hkv][blocks][max_rows]
     float *parts;                        // several rounds: [rounds][B][Hkv][part_stride], the sums over a round's rows, where the statistics were
-    float *rows;                         // [B][Hkv][max_rows]: log2 of a row's sum of exponentials
+    float2 *rows;                        // [B][Hkv][max_rows]: a row's maximum (log2 domain) and one over its sum
     int64_t score_stride, part_stride;
     float scale_log2e, decay;            // |scale| * log2(e)
     uint32_t q_flip;                     // 0x80008000 when scale < 0: every query element changes sign as it is loaded

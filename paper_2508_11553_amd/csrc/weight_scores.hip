@@ -545,15 +545,16 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
                 for (int i = 0; i < kRowTiles; ++i) {
                     const int end = masked ? row_end(a, s, first + i * kMaxGroup + n, rows) - t0 - half * kPage - 4 * (lane >> 4) : 0;
                     f32x4 x[kAtOnce];
-                    float m = -INFINITY, by[kAtOnce];   // by: what is left to multiply with
+                    float m = -INFINITY;
 #pragma unroll
                     for (int p = 0; p < kAtOnce; ++p) {
                         x[p] = products(k[p], q[i]);
-                        by[p] = masked ? 1.f : scale[p];
-                        if (masked)
+                        if (masked) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[p][e] = 16 * p + e < end ? x[p][e] * scale[p] : -INFINITY;
-                        m = max_of(m, by[p] * max_of(max_of(x[p][0], x[p][1]), x[p][2], x[p][3]));
+                            for (int e = 0; e < 4; ++e) m = fmaxf(m, 16 * p + e < end ? x[p][e] * scale[p] : -INFINITY);
+                        } else {
+                            m = max_of(m, scale[p] * max_of(max_of(x[p][0], x[p][1]), x[p][2], x[p][3]));
+                        }
                     }
                     if (__builtin_amdgcn_ballot_w64(m > stat[i].m + kSlack)) {   // wave-uniform
                         const Stat old = stat[i];
@@ -565,7 +566,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
                     for (int p = 0; p < kAtOnce; ++p)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], by[p], -ref));
+                            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[p][e], scale[p], -ref));   // (as in the second pass)
                             stat[i].l += !masked || 16 * p + e < end ? w : 0.f;
                         }
                 }
@@ -610,7 +611,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(WeightArgs a)
     if (slice == 0 && there) {
 #pragma unroll
         for (int i = 1; i < 4; ++i) sum = joined(sum, s_stat[i][threadIdx.x]);
-        a.rows[unit * a.max_rows + r] = sum.m + log2f(sum.l);
+        a.rows[unit * a.max_rows + r] = float2{sum.m, 1.f / sum.l};
     }
 }
 
@@ -624,9 +625,28 @@ SD_DEV float over_quarters(const float (&x)[4])
     return sum(__builtin_amdgcn_permlane16_swap(bits(u), bits(v), false, false));
 }
 
+// x of lane k of the wave's quarter that this lane is in (DPP row_newbcast; k a constant, below 8).
+SD_DEV float quarter_lane(float x, int k)
+{
+#define SD_LANE(k) \
+    case k: return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x150 + k, 0xf, 0xf, true))
+    switch (k) {
+        SD_LANE(0);
+        SD_LANE(1);
+        SD_LANE(2);
+        SD_LANE(3);
+        SD_LANE(4);
+        SD_LANE(5);
+        SD_LANE(6);
+    default:
+        SD_LANE(7);
+    }
+#undef SD_LANE
+}
+
 // Second step: the products once more, rows by tokens, so that a lane's sum runs over four rows of every tile and only the four quarters of the wave are
-// left to add; and the weights' sums over the rows.  Grid as in the first.  A row's statistics are one number, log2 of its sum of exponentials: a
-// maximum and a reciprocal take twice the registers, which spill (126 us against 88), but leave weights 1e-7 off on average, not 3e-7.
+// left to add; and the weights' sums over the rows.  Grid as in the first.  A row's weights are taken relative to its maximum and multiplied with one over its
+// sum, so their error does not grow with the scores; the factors of a lane's eight rows lie in one register of its quarter of the wave (in eight they spill).
 template <class K>
 __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightArgs a)
 {
@@ -645,14 +665,16 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
     const Stream<K> stream(a, b, g, page0, last, min(share.groups, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
     if (rows) {
         u32x4 q[kRowTiles][S];
-        float row[kRowTiles][4];   // of rows 4 (lane / 16) .. of each tile
+        float row[kRowTiles][4];   // maxima of rows 4 (lane / 16) .. of each tile
+        const int ni = first + n / 4 % kRowTiles * kMaxGroup + 4 * (lane >> 4) + n % 4;
+        const float inverse = ni < rows ? a.rows[unit * a.max_rows + ni].y : 0.f;   // of those rows: one each in lanes 0 .. 4 kRowTiles - 1 of the quarter
 #pragma unroll
         for (int i = 0; i < kRowTiles; ++i) {
             load_q<K>(q[i], a, s, g, first + i * kMaxGroup + n, rows, lane);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = first + i * kMaxGroup + 4 * (lane >> 4) + e;
-                row[i][e] = r < rows ? a.rows[unit * a.max_rows + r] : 0.f;
+                row[i][e] = r < rows ? a.rows[unit * a.max_rows + r].x : 0.f;
             }
         }
         stream.issue(0);
@@ -677,8 +699,9 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_apply_kernel(WeightA
                             const f32x4 x = products(q[i], k[p]);   // rows by tokens
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale[p], -row[i][e]));
-                                sum[half + p] += !masked || 16 * p < end[e] ? w : 0.f;
+                                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], scale[p], -row[i][e])), by = quarter_lane(inverse, 4 * i + e);
+                                if (masked) sum[half + p] += 16 * p < end[e] ? w * by : 0.f;
+                                else sum[half + p] = __builtin_fmaf(by, w, sum[half + p]);
                             }
                         }
                     }
