@@ -438,14 +438,17 @@ struct Stream {
     char *lds;          // [2][kGroupPages][K::kBytes]
     int ids, lane, wave, waves, groups;   // ids: of the workgroup's pages, a lane each
     float scales;
+    unsigned long long below_zero;   // of the pages: those whose scale is
     SD_DEV Stream(const WeightArgs &a, int b, int g, int page0, int last, int groups_, char *lds_, int lane_, int wave_, int waves_)
         : lds(lds_), lane(lane_), wave(wave_), waves(waves_), groups(groups_)
     {
         ids = a.block_table[(int64_t)b * a.max_blocks + min(page0 + lane, last)];
         scales = K::kScaled ? a.k_scales[(int64_t)ids * a.Hkv + g] * a.scale_log2e : a.scale_log2e;
+        below_zero = K::kScaled ? __builtin_amdgcn_ballot_w64(scales < 0.f) : 0;
         stride = (int64_t)a.Hkv * K::kBytes;
         pool = static_cast<const char *>(a.k_pages) + (int64_t)g * K::kBytes;
     }
+    SD_DEV bool any_below_zero(int group) const { return below_zero >> group * kGroupPages & ((1u << kGroupPages) - 1); }
     SD_DEV char *slot(int group, int i) const { return lds + ((group & 1) * kGroupPages + i) * K::kBytes; }
     SD_DEV void issue(int group) const
     {
@@ -573,7 +576,8 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
             }
         };
         if (first >= rows) continue;   // wave-uniform: rows that are not there
-        if (t0 + kGroupTokens <= s.base + 1) tiles(std::false_type{});   // every row attends all of these tokens
+        // every row attends all of these tokens, and of the scores of a page the largest comes from the largest product
+        if (t0 + kGroupTokens <= s.base + 1 && !stream.any_below_zero(group)) tiles(std::false_type{});
         else tiles(std::true_type{});
     }
 #pragma unroll
