@@ -481,8 +481,8 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
  * into the pages of new_block_table, so prefix pages that other trajectories
  * share stay as they are; the old pages are the caller's to release.  Keys
  * stay rotated to their own positions.
- * fp8 pools: a new tile's scale is the largest of its rows' old scales; rows
- * of a smaller one are re-encoded as code * (old / new), fp32, nearest e4m3fn.
+ * fp8 pools: a new tile's scale is the largest magnitude of its rows' old scales;
+ * rows of another one are re-encoded as code * (old / new), fp32, nearest e4m3fn.
  *
  *   sinks, recent      >= 0, sinks + recent <= budget
  *   scores             f32 [batch][num_kv_heads][score_stride]; score_stride at least max_context_len, a multiple of 4

@@ -7,7 +7,7 @@
 // Whole numbers throughout, so nothing depends on an order of additions.
 //
 // Move: a wave per (new page, KV head): 16 positions, their rows of K and V from wherever they lie, stored as one tile.  Bound by memory.
-// fp8: a new tile's scale is the largest of its rows' old scales, so a row from the tile of that scale keeps its codes and
+// fp8: a new tile's scale is the largest magnitude of its rows' old scales, so a row from the tile of that scale keeps its codes (or turns their signs) and
 // no other row can overflow; e4m3 codes are floating point, so a smaller row loses nothing but what falls below the smallest exponent.
 //
 // Measured (d = 128): 256 sequences and heads of 2 k - 64 k, bf16, 4096 stay: choice 40 us (one workgroup's walk over 64 k: load 14, digits 13, places 13),
@@ -228,10 +228,10 @@ struct Rows {
             if (r < n) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(to + r * ROW_BYTES + lane % kLanes * 16));
         }
     }
-    // Codes of rows whose scale was `old` (of lane r), under the largest of those; -> that.
-    SD_DEV float rescale(float old, int n, int lane)
+    // Codes of rows whose scale was `old` (of lane r; past the last row its own), under the largest magnitude of those; -> that.
+    SD_DEV float rescale(float old, int lane)
     {
-        float top = (lane & 15) < n ? old : 0.f;
+        float top = fabsf(old);
         for (int off = 1; off < 16; off *= 2) top = fmaxf(top, __shfl_xor(top, off, 64));
         const float ratio = top > 0.f ? old / top : 1.f;
 #pragma unroll
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a)
     kr.load(k, from, n, lane);
     vr.load(v, from, n, lane);
     if (FP8) {
-        const float ks = kr.rescale(a.k_scales[old_tile], n, lane), vs = vr.rescale(a.v_scales[old_tile], n, lane);
+        const float ks = kr.rescale(a.k_scales[old_tile], lane), vs = vr.rescale(a.v_scales[old_tile], lane);
         if (lane == 0) a.k_scales[tile] = ks, a.v_scales[tile] = vs;
     }
     kr.store(k + tile * kPage * kRow, n, lane);
