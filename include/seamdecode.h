@@ -458,8 +458,10 @@ int qk_norm_rope_backward(const sd_qk_norm *norm, const void *dq_out, const void
  *   scores_out   f32, the same layout; entries at positions >= L are left as they are
  *   score_stride at least max_context_len, a multiple of 4
  *   workspace    >= paged_weight_workspace_bytes(shape, max_q_len) bytes, contents ignored; never less for a
- *                larger batch, max_context_len or max_q_len.  It holds 4 bytes per row and token of the bound, rows
- *                (max_q_len times the heads of a group) counted as 4, 8 or 16, and what more rows need if that is more
+ *                larger batch, max_context_len or max_q_len.  With R = max_q_len times the heads of a group, a
+ *                sequence and KV head takes for R up to 16 (counted as 4, 8 or 16) about 4 R bytes per token of the bound;
+ *                for more the larger of that for 16 and 8 R bytes for every started 1024 tokens (every 64 where that comes to
+ *                less than 1 MB in all, which is added otherwise) or, above 256 rows, 4 bytes per token for every started 256; and 8 R
  */
 size_t paged_weight_workspace_bytes(const sd_shape *shape, int32_t max_q_len);
 int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t *q_start,

@@ -818,7 +818,7 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
         if (s->batch <= 64 && all <= 0x7fffffff) w.share = all;
     }
     w.block_tokens = sd::kPage * w.wave_tiles * (w.pack ? sd::kWaves * w.pack : 4);
-    w.blocks = parts(tokens, w.share ? 4 * sd::kPage : w.block_tokens);
+    w.blocks = parts(tokens, w.block_tokens);
     w.grid = w.share ? w.share : units * w.blocks * w.rounds;
     w.tiles = w.pack ? parts(tokens, w.pack * sd::kPage) : 0;
     w.apply_blocks = parts(tokens, 1024);
@@ -826,11 +826,20 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
     // The workspace is that of the most blocks, and of kept products though one kernel may do without or there are too many rows: a caller's, sized
     // for its largest batch, longest sequences and most query rows, serves every smaller call.
     const auto layout = [&](int64_t rows) {
-        const int pack = rows <= sd::kMaxGroup ? sd::weight_pack(rows) : 0;
-        const int64_t most_blocks = parts(tokens, pack ? sd::kPage * sd::kWaves * pack * parts(2, pack) : 4 * sd::kPage);
-        w.stats_off = pack ? up((size_t)units * parts(tokens, pack * sd::kPage) * 1024) : 0;
-        w.rows_off = w.stats_off + up((size_t)units * most_blocks * (pack ? sd::kMaxGroup / pack : rows) * 8);
-        return w.rows_off + (pack ? 0 : up((size_t)units * rows * 8));
+        if (rows <= sd::kMaxGroup) {
+            const int pack = sd::weight_pack(rows);
+            w.stats_off = up((size_t)units * parts(tokens, pack * sd::kPage) * 1024);
+            w.rows_off = w.stats_off + up((size_t)units * parts(tokens, sd::kPage * sd::kWaves * pack * parts(2, pack)) * (sd::kMaxGroup / pack) * 8);
+            return w.rows_off;
+        }
+        // Statistics: a stretch has 64 tokens at least; and there are no more of them than workgroups to a round of rows, those that kMaxGroups groups each ask for
+        // and less than one turn besides, whose workgroups hold 16 waves' rows on every compute unit.  The rounds' sums take their place.
+        constexpr int64_t kTurnRows = (int64_t)kMaxRangeWorkgroups / 2 * 16 * sd::kRowsOfWave;
+        const size_t each = (size_t)units * rows, stats = std::min(each * parts(tokens, 4 * sd::kPage), each * parts(tokens, 4 * sd::kPage * sd::kMaxGroups) + kTurnRows);
+        const int64_t rounds = parts(rows, sd::row_waves(rows) * sd::kRowsOfWave);
+        w.stats_off = 0;
+        w.rows_off = up(std::max(stats * 8, rounds > 1 ? (size_t)units * rounds * parts(tokens, 4) * 16 : 0));
+        return w.rows_off + up(each * 8);
     };
     const int64_t group = s->num_q_heads / s->num_kv_heads;
     const size_t fewer = layout(std::min(w.rows, sd::kMaxGroup / group * group));

@@ -656,7 +656,7 @@ struct WeightArgs {
     const float *scores_in;              // [B][Hkv][score_stride]; null: zeros
     float *scores_out;
     float *products;                     // [B][Hkv][max_tiles][64 lanes][4]: a decode step's, log2 domain
-    float2 *stats;                       // (max, sum) of a row over a stretch of tokens.  Products kept: [B][Hkv][blocks][16 / pack], else [B][Hkv][blocks][max_rows]
+    float2 *stats;                       // (max, sum) of a row over a stretch of tokens.  Products kept: [B][Hkv][blocks][16 / pack], else [stretches][Hkv][max_rows], sequence by sequence
     float *parts;                        // several rounds: [rounds][B][Hkv][part_stride], the sums over a round's rows, where the statistics were
     float2 *rows;                        // [B][Hkv][max_rows]: a row's maximum (log2 domain) and one over its sum
     int64_t score_stride, part_stride;

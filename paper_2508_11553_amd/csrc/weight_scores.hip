@@ -479,6 +479,7 @@ struct Stream {
 // as even as if all lengths were the bound's.  8 sequences of 5 k - 8 k, 256 rows, 8 KV heads: 13 groups each, not 16.
 struct Share {
     int b, c, groups;   // b < 0: none
+    int slot;           // of the statistics: sequence by sequence, a stretch of tokens each
 };
 SD_DEV int lane_groups(const WeightArgs &a, int lane) { return lane < a.B ? (max(0, min(a.context_lens[lane], a.max_context_len)) + kGroupTokens - 1) / kGroupTokens : 0; }
 SD_DEV int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
@@ -493,11 +494,18 @@ SD_DEV int share_groups(const WeightArgs &a, int mine)
 SD_DEV Share share_of(const WeightArgs &a, int lane)
 {
     const int at = blockIdx.x / (a.Hkv * a.rounds);
-    if (a.share == 0) return Share{at / a.blocks, at % a.blocks, a.wave_tiles};
+    if (a.share == 0) return Share{at / a.blocks, at % a.blocks, a.wave_tiles, at};
     const int mine = lane_groups(a, lane), w = share_groups(a, mine), parts = (mine + w - 1) / w, upto = wave_scan(parts);
     const int b = __builtin_popcountll(__builtin_amdgcn_ballot_w64(upto <= at));
-    if (b >= 64) return Share{-1, 0, 0};
-    return Share{b, at - __builtin_amdgcn_readlane(upto - parts, b), w};
+    if (b >= 64) return Share{-1, 0, 0, 0};
+    return Share{b, at - __builtin_amdgcn_readlane(upto - parts, b), w, at};
+}
+// The first slot of sequence b, and its stretches' tokens.
+SD_DEV Share first_share(const WeightArgs &a, int b, int lane)
+{
+    if (a.share == 0) return Share{b, 0, a.wave_tiles, b * a.blocks};
+    const int mine = lane_groups(a, lane), w = share_groups(a, mine), parts = (mine + w - 1) / w;
+    return Share{b, 0, w, __builtin_amdgcn_readlane(wave_scan(parts) - parts, b)};
 }
 
 template <int STEPS>
@@ -526,7 +534,7 @@ __global__ __launch_bounds__(kRowWaves * 64, 4) void weight_stats_kernel(WeightA
     const int first = (blockIdx.x / a.Hkv % a.rounds * waves + wave) * kRowsOfWave;   // the wave's first row
     if (page0 > last || first - wave * kRowsOfWave >= rows) return;   // (L == 0: last is -1)
     const Stream<K> stream(a, b, g, page0, last, min(share.groups, (last - page0) / kGroupPages + 1), s_pages, lane, wave, waves);
-    float2 *stats = a.stats + (((int64_t)b * a.Hkv + g) * a.blocks + c) * a.max_rows;
+    float2 *stats = a.stats + ((int64_t)share.slot * a.Hkv + g) * a.max_rows;
     u32x4 q[kRowTiles][S];
     Stat stat[kRowTiles];
 #pragma unroll
@@ -597,14 +605,16 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(WeightArgs a)
     __shared__ Stat s_stat[4][64];
     const Sequence s = sequence_of(a, (int)(unit / a.Hkv));
     const bool there = r < s.n * a.G;
-    const int lane = threadIdx.x & 63, tokens = share_groups(a, a.share ? lane_groups(a, lane) : 0) * kGroupTokens, blocks = (s.L + tokens - 1) / tokens;
+    const Share share = first_share(a, (int)(unit / a.Hkv), threadIdx.x & 63);
+    const int tokens = share.groups * kGroupTokens, blocks = (s.L + tokens - 1) / tokens;
+    const int64_t step = (int64_t)a.Hkv * a.max_rows;   // from a stretch to the next
     Stat sum = {-INFINITY, 0.f};
     if (there) {
-        const float2 *v = a.stats + unit * a.blocks * a.max_rows + r;
+        const float2 *v = a.stats + share.slot * step + unit % a.Hkv * a.max_rows + r;
         for (int c = slice; c < blocks; c += 32) {
             float2 w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = v[(int64_t)min(c + 4 * i, blocks - 1) * a.max_rows];
+            for (int i = 0; i < 8; ++i) w[i] = v[min(c + 4 * i, blocks - 1) * step];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (c + 4 * i < blocks) sum = joined(sum, Stat{w[i].x, w[i].y});
