@@ -1046,7 +1046,7 @@ int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recen
     a.recent = recent;
     a.new_pages = std::max(1, (most + sd::kPage - 1) / sd::kPage);
     const uint64_t units = (uint64_t)a.B * a.Hkv;
-    if (too_many_threads(units, 1024) || too_many_threads(units * a.new_pages, 64)) return SD_EUNSUPPORTED;   // the choice, the move
+    if (too_many_threads(units, 1024) || too_many_threads((units * a.new_pages + 3) / 4, 256)) return SD_EUNSUPPORTED;   // the choice, the move: a wave to a page, four to a workgroup
     const hipError_t e = sd::launch_evict(a, shape->head_dim, shape->kv_dtype, static_cast<hipStream_t>(stream));
     if (e == hipErrorNotSupported) return SD_EUNSUPPORTED;
     return e == hipSuccess ? SD_OK : hip_fail(e);
