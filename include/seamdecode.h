@@ -457,6 +457,7 @@ int qk_norm_rope_backward(const sd_qk_norm *norm, const void *dq_out, const void
  *   scores_in    f32 [batch][num_kv_heads][score_stride], or NULL: zeros; may be scores_out
  *   scores_out   f32, the same layout; entries at positions >= L are left as they are
  *   score_stride at least max_context_len, a multiple of 4
+ *   max_context_len (of shape) up to 2^31 - 65536 (SD_EUNSUPPORTED beyond)
  *   workspace    >= paged_weight_workspace_bytes(shape, max_q_len) bytes, contents ignored; never less for a
  *                larger batch, max_context_len or max_q_len.  With R = max_q_len times the heads of a group, a
  *                sequence and KV head takes for R up to 16 (counted as 4, 8 or 16) about 4 R bytes per token of the bound;
@@ -496,6 +497,7 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
  *   scores_out         f32 [batch][num_kv_heads][scores_out_stride] or NULL: the kept tokens'
  *                      scores in their new places; stride >= min(budget, max_context_len);
  *                      may be scores (equal strides)
+ *   max_context_len    (of shape) up to 2^31 - 65536 (SD_EUNSUPPORTED beyond)
  */
 int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recent,
              const float *scores, int64_t score_stride,

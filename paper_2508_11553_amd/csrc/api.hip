@@ -956,6 +956,7 @@ int paged_weight_accumulate(const sd_shape *shape, const void *q, const int32_t 
         (q_start && !aligned16(q_start)) || (scores_in && !aligned16(scores_in)))
         return SD_EINVAL;
     if (shape->kv_dtype == SD_FP8_E4M3 && bad_ptr(k_scales)) return SD_EINVAL;
+    if (shape->max_context_len > sd::kMaxWalk) return SD_EUNSUPPORTED;
     max_q_len = std::min(max_q_len, total_q);
     const uint64_t units = (uint64_t)shape->batch * shape->num_kv_heads;
     if (too_many_threads(units, 1024)) return SD_EUNSUPPORTED;
@@ -1023,6 +1024,7 @@ int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recen
         return SD_EINVAL;
     const bool fp8 = shape->kv_dtype == SD_FP8_E4M3;
     if (fp8 && (bad_ptr(k_scales) || bad_ptr(v_scales))) return SD_EINVAL;
+    if (shape->max_context_len > sd::kMaxWalk) return SD_EUNSUPPORTED;
     sd::EvictArgs a;
     a.scores = scores;
     a.scores_out = scores_out;

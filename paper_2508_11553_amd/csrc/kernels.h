@@ -602,6 +602,8 @@ __host__ inline Division division_by(uint32_t by)
     return Division{(uint32_t)((((uint64_t)1 << (31 + l)) / by) + 1), (uint32_t)(l - 1)};
 }
 constexpr uint64_t kMaxThreads = 0xffffffff;   // of one launch
+// Tokens of a sequence that the accumulated weights and the eviction walk: by up to 65536 at a time, counted in 32 bits past the last one.
+constexpr int32_t kMaxWalk = 0x7fff0000;
 
 // Rows of the norm and rotation (norm_rope.hip): x rows of q and k at strides, y rows contiguous.
 struct NormRopeArgs {
