@@ -11,8 +11,9 @@
 // 64 to 256, between two launches (weight_products_kernel, weight_apply_kept_kernel).  Bound by reading K: 256 of 1 k - 8 k, bf16, 7 heads a group:
 // 61 us, 4.4 TB/s of the 6.7 that a plain walk reads, for the longest of a compute unit's sequences ends last; 2048 of 0.5 k - 4 k, fp8: 117 us, 5.3 TB/s.
 // With more rows (the last tokens of a prompt) the products would be more bytes than K: they are made twice, by weight_stats_kernel and
-// weight_apply_kernel, rows stay in registers and K streams past.  Bound by the exponentials and what surrounds them: 8 sequences of 5 k - 8 k,
-// 8 KV heads, 256 rows 41 + 5 + 39 us, 650 and 690 TFLOP/s in the passes; vector units 61 - 68 % busy, matrix units 35 %, both at once 13 %.
+// weight_apply_kernel, rows stay in registers and K streams past.  Bound by matrix and vector units taking turns, for the waves of a workgroup do the same
+// thing at the same time: 8 sequences of 5 k - 8 k, 8 KV heads, 256 rows 41 + 5 + 40 us, 660 and 670 TFLOP/s in the passes; vector units 62 - 69 % busy, matrix
+// units 34 %, both at once 11 - 13 %.
 //
 // Where products are kept a lane holds four tokens (4 (lane / 16) ..) of row lane % 16.  Which d an operand's 16 bytes are differs between
 // pools, and Q is read in the same order.  Weights, sums and scores are fp32 throughout.
