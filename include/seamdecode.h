@@ -59,7 +59,7 @@ struct sd_timer; /* see the measurement aids at the end */
 
 #define SD_BF16 0
 #define SD_FP8_E4M3 1
-#define SD_F32 2 /* norm weights only (sd_qk_norm) */
+#define SD_F32 2 /* norm weights (sd_qk_norm) and logits (sd_logits) only */
 
 typedef struct {
     int32_t batch;              /* B >= 0 (0: the call is a no-op) */
@@ -505,6 +505,128 @@ int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recen
              const int32_t *block_table, const int32_t *context_lens,
              const int32_t *new_block_table, int32_t *kept, int32_t *new_lens,
              float *scores_out, int64_t scores_out_stride, void *stream);
+
+/*
+ * Rows of logits, what sample_tokens draws from and token_logprobs scores.
+ */
+typedef struct {
+    int32_t rows;    /* >= 0 (0: the call is a no-op) */
+    int32_t vocab;   /* logits of a row, >= 1 */
+    int32_t dtype;   /* SD_BF16 or SD_F32 */
+    int64_t stride;  /* elements between two rows, at least vocab, any number; 0: rows lie side by side */
+} sd_logits;
+
+/*
+ * sample_tokens -- a token for every row of logits.
+ *
+ * The end of a decode step (a rollout advances token by token).  With x a row's logits, T its temperature,
+ * z = x / T and w = exp(z - max z), a row keeps, counted from the largest logit down and of equal logits
+ * from the lower index up,
+ *     its first top_k tokens,
+ *     of those the shortest beginning that holds the share top_p of their weight (at least one),
+ *     of those the ones with w >= min_p,
+ * and draws the first token, by index, for which the weight of the kept tokens up to it
+ * exceeds uniform times the weight of all that are kept.  Weights are rounded to multiples of 2^-43
+ * and their sums exact: a row's token depends on nothing but the row and its parameters,
+ * not on the batch around it, and is the same in every call.
+ *
+ *   temperature     f32 [rows] or NULL: 1.  0, negative or NaN: the largest logit is taken, of equal ones
+ *                   the first; the log probabilities are those of T = 1 and draw_logprobs 0
+ *   top_k           i32 [rows] or NULL; <= 0 or >= vocab: no limit
+ *   top_p           f32 [rows] or NULL; >= 1 or NaN: no limit; <= 0: one token
+ *   min_p           f32 [rows] or NULL; <= 0 or NaN: no limit; >= 1: the largest logits alone
+ *   uniform         f32 [rows], in [0, 1); below (or NaN) counts as 0, from 1 on as just below 1
+ *   tokens          i32 [rows], written
+ *   logprobs        f32 [rows] or NULL: log(w / sum of all w), the token's log probability at the
+ *                   row's temperature; what token_logprobs gives for it
+ *   draw_logprobs   f32 [rows] or NULL: log(w / sum of the kept w), that of the draw
+ *   workspace       >= sample_workspace_bytes(logits) bytes, contents ignored
+ * -inf (and NaN) is never drawn.  +inf: the tokens that have it share all weight.  A row with no
+ * logit above -inf gives token -1 and log probabilities of -inf.  vocab < 2^20 (SD_EUNSUPPORTED beyond).
+ */
+size_t sample_workspace_bytes(const sd_logits *shape);
+int sample_tokens(const sd_logits *shape, const void *logits, const float *temperature, const int32_t *top_k,
+                  const float *top_p, const float *min_p, const float *uniform,
+                  int32_t *tokens, float *logprobs, float *draw_logprobs,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * token_logprobs -- log probabilities of given tokens, with the entropy of every row.
+ *
+ * What training makes of a rollout's tokens.  With z = x / T and S = sum exp(z - max z):
+ *     logprobs = z_target - max z - log S,   entropy = -sum p log p
+ * in fp32.
+ *
+ *   targets       i32 [rows]; a row whose target is outside [0, vocab) is padding: its logits are not
+ *                 read, its results are 0
+ *   temperature   f32 [rows] or NULL: 1; 0, negative and NaN count as 1
+ *   entropy       f32 [rows] or NULL
+ *   stats         f32 [rows][2] or NULL: what the gradient needs
+ *   workspace     >= token_logprobs_workspace_bytes(shape) bytes, contents ignored; the same for
+ *                 every shape
+ * A target of -inf has the log probability -inf; a row of nothing else -inf and the entropy 0; NaN or +inf in a row
+ * makes its results NaN.  vocab < 2^30 (SD_EUNSUPPORTED beyond).
+ */
+size_t token_logprobs_workspace_bytes(const sd_logits *shape);
+int token_logprobs(const sd_logits *shape, const void *logits, const int32_t *targets, const float *temperature,
+                   float *logprobs, float *entropy, float *stats,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * token_logprobs_backward -- the gradient of token_logprobs, from its inputs, its stats and entropy, and the
+ * gradients g of its log probabilities and h of its entropies:
+ *     dx_j = (g ([j == target] - p_j) - h p_j (log p_j + entropy)) / T
+ * rounded to the logits' type once.
+ *
+ *   entropy, d_entropy   f32 [rows], or both NULL: h is 0
+ *   d_logits             laid out as logits (their stride; what lies between two rows stays as it is);
+ *                        may be logits themselves
+ * Rows of padding, and those with no logit above -inf, get zeros.
+ */
+int token_logprobs_backward(const sd_logits *shape, const void *logits, const int32_t *targets, const float *temperature,
+                            const float *stats, const float *entropy, const float *d_logprobs, const float *d_entropy,
+                            void *d_logits, void *stream);
+
+/*
+ * kv_plan_step -- places for the new tokens of every sequence, on the device.
+ *
+ * Before rows go into the cache somebody has to find pages for them and to say where each goes.  For every
+ * sequence b with L = context_lens_in[b] tokens (clamped to [0, max_context_len]) and n = new_tokens[b]:
+ *     n > 0   the sequence gets n slots behind its last one, and pages for them where its last page does
+ *             not hold them: block_table[b] grows, its length becomes L + n
+ *     n == 0  it waits: nothing changes
+ *     n < 0   it is finished: its pages go back on the free list (those of its first shared_len[b] / 16
+ *             full pages excepted, which are not its own), its length becomes 0; its table row stays as it is
+ * Pages that come back are free for this call's other sequences.  Sequences are served in the batch's order: with all that was asked
+ * for up to and including b summed up, b gets its slots if the free pages suffice (or it needs
+ * none) and its rows fit max_rows; else, and where L + n exceeds max_context_len, it waits.
+ *
+ *   new_tokens          i32 [batch]
+ *   shared_len          i32 [batch] or NULL: zeros
+ *   context_lens_in     i32 [batch];  context_lens_out may be the same
+ *   next_in, next_out   i32 [batch], or both NULL: the position of the next token where it is not the length
+ *                       (a cache that was cut down, kv_evict); may be the same
+ *   free_pages          i32 [num_pages]: a stack of free pages, of which the first free_in[0] count.  Pages are taken from its top
+ *                       (those that come back lie on it, in the batch's order); entries below free_in[0]
+ *                       are not written
+ *   free_in, free_out   i32 [1]; may be the same
+ *   block_table         i32 [batch][max_blocks_per_seq]; entries of new pages are written, others stay
+ *   granted             i32 [batch], written: n where b got its slots, else 0
+ *   row_start           i32 [batch + 1], written: b's rows are row_start[b] .. row_start[b + 1] - 1; the q_start of
+ *                       paged_prefill_attention, the range_row0 of kv_append_fp8
+ *   starts              i32 [batch], written: L; the range_start of kv_append_fp8
+ *   seq_ids, slots, positions   i32 [max_rows], written: what qk_norm_rope_append takes; rows that no sequence has get -1, 0
+ *                       and 0.  positions may be NULL
+ *   workspace           >= kv_plan_workspace_bytes(shape) bytes, contents ignored; never less for a larger batch
+ * Where free pages suffice for all and every sequence's pages are its own, tables and free list together always hold every page once.
+ * Of shape only batch, num_pages, max_blocks_per_seq and max_context_len are used.  batch < 2^24 (SD_EUNSUPPORTED beyond).
+ */
+size_t kv_plan_workspace_bytes(const sd_shape *shape);
+int kv_plan_step(const sd_shape *shape, const int32_t *new_tokens, const int32_t *shared_len,
+                 const int32_t *context_lens_in, int32_t *context_lens_out, const int32_t *next_in, int32_t *next_out,
+                 int32_t *free_pages, const int32_t *free_in, int32_t *free_out, int32_t *block_table, int32_t max_rows,
+                 int32_t *granted, int32_t *row_start, int32_t *starts, int32_t *seq_ids, int32_t *slots, int32_t *positions,
+                 void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Session prefix tree (host only; no device memory, no HIP calls).

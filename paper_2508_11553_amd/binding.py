@@ -53,6 +53,16 @@ class QkNorm(ctypes.Structure):
     ]
 
 
+class Logits(ctypes.Structure):
+    """Mirror of sd_logits."""
+    _fields_ = [
+        ("rows", ctypes.c_int32),
+        ("vocab", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("stride", ctypes.c_int64),
+    ]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -115,6 +125,21 @@ def load():
     L.paged_weight_accumulate.argtypes = [sp, vp, vp, i32, i32, vp, vp, vp, vp, f32, f32, i32, vp, vp, i64, vp, sz, vp]
     L.kv_evict.restype = ctypes.c_int
     L.kv_evict.argtypes = [sp, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lp = ctypes.POINTER(Logits)
+    L.sample_workspace_bytes.restype = sz
+    L.sample_workspace_bytes.argtypes = [lp]
+    L.sample_tokens.restype = ctypes.c_int
+    L.sample_tokens.argtypes = [lp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.token_logprobs_workspace_bytes.restype = sz
+    L.token_logprobs_workspace_bytes.argtypes = [lp]
+    L.token_logprobs.restype = ctypes.c_int
+    L.token_logprobs.argtypes = [lp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.token_logprobs_backward.restype = ctypes.c_int
+    L.token_logprobs_backward.argtypes = [lp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.kv_plan_workspace_bytes.restype = sz
+    L.kv_plan_workspace_bytes.argtypes = [sp]
+    L.kv_plan_step.restype = ctypes.c_int
+    L.kv_plan_step.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.sd_validate_tables.restype = ctypes.c_int
     L.sd_validate_tables.argtypes = [sp, vp, vp, vp, vp]
     L.sd_validate_groups.restype = ctypes.c_int
@@ -358,6 +383,52 @@ def kv_evict(shape: Shape, budget: int, sinks: int, recent: int, scores, score_s
                          _ptr(context_lens), _ptr(new_block_table), _ptr(kept), _ptr(new_lens), _ptr(scores_out),
                          int(scores_out_stride), _stream(stream))
     _check(rc, "kv_evict")
+
+
+def sample_workspace_bytes(shape: Logits) -> int:
+    return int(load().sample_workspace_bytes(ctypes.byref(shape)))
+
+
+def sample_tokens(shape: Logits, logits, temperature, top_k, top_p, min_p, uniform, tokens, logprobs, draw_logprobs,
+                  workspace, workspace_nbytes: int, stream=None):
+    rc = load().sample_tokens(ctypes.byref(shape), _ptr(logits), _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                              _ptr(min_p), _ptr(uniform), _ptr(tokens), _ptr(logprobs), _ptr(draw_logprobs),
+                              _ptr(workspace), int(workspace_nbytes), _stream(stream))
+    _check(rc, "sample_tokens")
+
+
+def token_logprobs_workspace_bytes(shape: Logits) -> int:
+    return int(load().token_logprobs_workspace_bytes(ctypes.byref(shape)))
+
+
+def token_logprobs(shape: Logits, logits, targets, temperature, logprobs, entropy, stats, workspace,
+                   workspace_nbytes: int, stream=None):
+    rc = load().token_logprobs(ctypes.byref(shape), _ptr(logits), _ptr(targets), _ptr(temperature), _ptr(logprobs),
+                               _ptr(entropy), _ptr(stats), _ptr(workspace), int(workspace_nbytes), _stream(stream))
+    _check(rc, "token_logprobs")
+
+
+def token_logprobs_backward(shape: Logits, logits, targets, temperature, stats, entropy, d_logprobs, d_entropy,
+                            d_logits, stream=None):
+    rc = load().token_logprobs_backward(ctypes.byref(shape), _ptr(logits), _ptr(targets), _ptr(temperature),
+                                        _ptr(stats), _ptr(entropy), _ptr(d_logprobs), _ptr(d_entropy), _ptr(d_logits),
+                                        _stream(stream))
+    _check(rc, "token_logprobs_backward")
+
+
+def kv_plan_workspace_bytes(shape: Shape) -> int:
+    return int(load().kv_plan_workspace_bytes(ctypes.byref(shape)))
+
+
+def kv_plan_step(shape: Shape, new_tokens, shared_len, context_lens_in, context_lens_out, next_in, next_out, free_pages,
+                 free_in, free_out, block_table, max_rows: int, granted, row_start, starts, seq_ids, slots, positions,
+                 workspace, workspace_nbytes: int, stream=None):
+    rc = load().kv_plan_step(ctypes.byref(shape), _ptr(new_tokens), _ptr(shared_len), _ptr(context_lens_in),
+                             _ptr(context_lens_out), _ptr(next_in), _ptr(next_out), _ptr(free_pages), _ptr(free_in),
+                             _ptr(free_out), _ptr(block_table), int(max_rows), _ptr(granted), _ptr(row_start),
+                             _ptr(starts), _ptr(seq_ids), _ptr(slots), _ptr(positions), _ptr(workspace),
+                             int(workspace_nbytes), _stream(stream))
+    _check(rc, "kv_plan_step")
 
 
 def validate_tables(shape: Shape, block_table, context_lens, report, stream=None):

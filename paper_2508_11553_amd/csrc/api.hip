@@ -847,6 +847,47 @@ WeightPlan weight_plan(const sd_shape *s, int32_t max_q_len)
     return w;
 }
 
+constexpr int32_t kMaxScoredVocab = (1 << 30) - 1;
+constexpr int kLogprobParts = 1024;   // of a call whose rows are cut
+
+int check_logits(const sd_logits *s, int32_t max_vocab)
+{
+    if (!s || s->rows < 0 || s->vocab < 1 || (s->stride != 0 && s->stride < s->vocab)) return SD_EINVAL;
+    if (s->dtype != SD_BF16 && s->dtype != SD_F32) return SD_EINVAL;
+    if (s->vocab > max_vocab || s->stride > ((int64_t)1 << 40)) return SD_EUNSUPPORTED;
+    return SD_OK;
+}
+
+// 16-byte vectors that a row reaches into, at most.
+int64_t row_vectors(const sd_logits *s)
+{
+    const int each = s->dtype == SD_F32 ? 4 : 8;
+    return ((int64_t)s->vocab + 2 * each - 2) / each;
+}
+
+// No heads and no rows of the pools enter.
+int check_plan(const sd_shape *s)
+{
+    if (!s || s->batch < 0 || s->num_pages < 0 || s->max_blocks_per_seq <= 0 || s->max_context_len < 0 || s->page_size != sd::kPage) return SD_EINVAL;
+    if ((int64_t)s->max_context_len > (int64_t)sd::kPage * s->max_blocks_per_seq) return SD_EINVAL;
+    if (s->batch >= 1 << 24) return SD_EUNSUPPORTED;
+    return SD_OK;
+}
+
+struct PlanLayout {
+    size_t page_off, next_off, count_off, total;
+};
+PlanLayout plan_layout(const sd_shape *s)
+{
+    const size_t entries = ((size_t)s->batch + 4) & ~(size_t)3;   // batch + 1, to 16 bytes
+    PlanLayout w;
+    w.page_off = entries * 8;
+    w.next_off = w.page_off + entries * 4;
+    w.count_off = w.next_off + entries * 4;
+    w.total = w.count_off + 16;
+    return w;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1051,6 +1092,150 @@ int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recen
     if (too_many_threads(units, 1024) || too_many_threads((units * a.new_pages + 3) / 4, 256)) return SD_EUNSUPPORTED;   // the choice, the move: a wave to a page, four to a workgroup
     const hipError_t e = sd::launch_evict(a, shape->head_dim, shape->kv_dtype, static_cast<hipStream_t>(stream));
     if (e == hipErrorNotSupported) return SD_EUNSUPPORTED;
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+size_t sample_workspace_bytes(const sd_logits *shape)
+{
+    return check_logits(shape, sd::kMaxVocab) ? 0 : 256;
+}
+
+int sample_tokens(const sd_logits *shape, const void *logits, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                  const float *uniform, int32_t *tokens, float *logprobs, float *draw_logprobs, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_logits(shape, sd::kMaxVocab);
+    if (rc) return rc;
+    if (shape->rows == 0) return SD_OK;
+    if (bad_ptr(logits) || bad_ptr(uniform) || bad_ptr(tokens) || bad_ptr(workspace) || !aligned16(temperature) || !aligned16(top_k) || !aligned16(top_p) ||
+        !aligned16(min_p) || !aligned16(logprobs) || !aligned16(draw_logprobs))
+        return SD_EINVAL;
+    if (too_many_threads(shape->rows, 1024)) return SD_EUNSUPPORTED;
+    if (workspace_bytes < sample_workspace_bytes(shape)) return SD_EWORKSPACE;
+    sd::SampleArgs a;
+    a.logits = logits;
+    a.stride = shape->stride ? shape->stride : shape->vocab;
+    a.rows = shape->rows;
+    a.vocab = shape->vocab;
+    a.temperature = temperature;
+    a.top_k = top_k;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.uniform = uniform;
+    a.tokens = tokens;
+    a.logprobs = logprobs;
+    a.draw_logprobs = draw_logprobs;
+    const hipError_t e = sd::launch_sample(a, shape->dtype == SD_F32, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+size_t token_logprobs_workspace_bytes(const sd_logits *shape)
+{
+    return check_logits(shape, kMaxScoredVocab) ? 0 : (size_t)kLogprobParts * 3 * 4;
+}
+
+int token_logprobs(const sd_logits *shape, const void *logits, const int32_t *targets, const float *temperature, float *logprobs, float *entropy, float *stats,
+                   void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_logits(shape, kMaxScoredVocab);
+    if (rc) return rc;
+    if (shape->rows == 0) return SD_OK;
+    if (bad_ptr(logits) || bad_ptr(targets) || bad_ptr(logprobs) || bad_ptr(workspace) || !aligned16(temperature) || !aligned16(entropy) || !aligned16(stats)) return SD_EINVAL;
+    if (workspace_bytes < token_logprobs_workspace_bytes(shape)) return SD_EWORKSPACE;
+    sd::LogprobArgs a;
+    a.logits = logits;
+    a.stride = shape->stride ? shape->stride : shape->vocab;
+    a.rows = shape->rows;
+    a.vocab = shape->vocab;
+    a.targets = targets;
+    a.temperature = temperature;
+    a.logprobs = logprobs;
+    a.entropy = entropy;
+    a.stats = stats;
+    a.parts = static_cast<float *>(workspace);
+    a.slices = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kLogprobParts / shape->rows, row_vectors(shape) / 1024));
+    a.per_row = sd::division_by(a.slices);
+    if (too_many_threads((uint64_t)a.rows * a.slices, 512)) return SD_EUNSUPPORTED;
+    const hipError_t e = sd::launch_logprobs(a, shape->dtype == SD_F32, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+int token_logprobs_backward(const sd_logits *shape, const void *logits, const int32_t *targets, const float *temperature, const float *stats, const float *entropy,
+                            const float *d_logprobs, const float *d_entropy, void *d_logits, void *stream)
+{
+    const int rc = check_logits(shape, kMaxScoredVocab);
+    if (rc) return rc;
+    if (shape->rows == 0) return SD_OK;
+    if (bad_ptr(logits) || bad_ptr(targets) || bad_ptr(stats) || bad_ptr(d_logprobs) || bad_ptr(d_logits) || !aligned16(temperature) || !aligned16(entropy) ||
+        !aligned16(d_entropy) || !entropy != !d_entropy)
+        return SD_EINVAL;
+    sd::LogprobGradArgs a;
+    a.logits = logits;
+    a.stride = shape->stride ? shape->stride : shape->vocab;
+    a.rows = shape->rows;
+    a.vocab = shape->vocab;
+    a.targets = targets;
+    a.temperature = temperature;
+    a.stats = stats;
+    a.entropy = entropy;
+    a.d_logprobs = d_logprobs;
+    a.d_entropy = d_entropy;
+    a.d_logits = d_logits;
+    a.slices = (int32_t)((row_vectors(shape) + 256 * sd::kGradVectors - 1) / (256 * sd::kGradVectors));
+    a.per_row = sd::division_by(a.slices);
+    if (too_many_threads((uint64_t)a.rows * a.slices, 256)) return SD_EUNSUPPORTED;
+    const hipError_t e = sd::launch_logprobs_backward(a, shape->dtype == SD_F32, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SD_OK : hip_fail(e);
+}
+
+size_t kv_plan_workspace_bytes(const sd_shape *shape)
+{
+    if (check_plan(shape)) return 0;
+    return plan_layout(shape).total;
+}
+
+int kv_plan_step(const sd_shape *shape, const int32_t *new_tokens, const int32_t *shared_len, const int32_t *context_lens_in, int32_t *context_lens_out,
+                 const int32_t *next_in, int32_t *next_out, int32_t *free_pages, const int32_t *free_in, int32_t *free_out, int32_t *block_table, int32_t max_rows,
+                 int32_t *granted, int32_t *row_start, int32_t *starts, int32_t *seq_ids, int32_t *slots, int32_t *positions, void *workspace,
+                 size_t workspace_bytes, void *stream)
+{
+    const int rc = check_plan(shape);
+    if (rc) return rc;
+    if (max_rows < 0) return SD_EINVAL;
+    if (shape->batch == 0) return SD_OK;
+    if (bad_ptr(new_tokens) || !aligned16(shared_len) || bad_ptr(context_lens_in) || bad_ptr(context_lens_out) || !aligned16(next_in) || !aligned16(next_out) ||
+        !next_in != !next_out || bad_ptr(free_pages) || bad_ptr(free_in) || bad_ptr(free_out) || bad_ptr(block_table) || bad_ptr(granted) || bad_ptr(row_start) ||
+        bad_ptr(starts) || bad_ptr(workspace) || (max_rows > 0 && (bad_ptr(seq_ids) || bad_ptr(slots) || !aligned16(positions))))
+        return SD_EINVAL;
+    const PlanLayout w = plan_layout(shape);
+    if (workspace_bytes < w.total) return SD_EWORKSPACE;
+    char *ws = static_cast<char *>(workspace);
+    sd::PlanArgs a;
+    a.new_tokens = new_tokens;
+    a.shared_len = shared_len;
+    a.lens_in = context_lens_in;
+    a.lens_out = context_lens_out;
+    a.next_in = next_in;
+    a.next_out = next_out;
+    a.free_pages = free_pages;
+    a.free_in = free_in;
+    a.free_out = free_out;
+    a.block_table = block_table;
+    a.granted = granted;
+    a.row_start = row_start;
+    a.starts = starts;
+    a.seq_ids = seq_ids;
+    a.slots = slots;
+    a.positions = positions;
+    a.back_from = reinterpret_cast<int64_t *>(ws);
+    a.page_from = reinterpret_cast<int32_t *>(ws + w.page_off);
+    a.next_at = reinterpret_cast<int32_t *>(ws + w.next_off);
+    a.counts = reinterpret_cast<int32_t *>(ws + w.count_off);
+    a.B = shape->batch;
+    a.max_blocks = shape->max_blocks_per_seq;
+    a.num_pages = shape->num_pages;
+    a.max_context_len = shape->max_context_len;
+    a.max_rows = max_rows;
+    const hipError_t e = sd::launch_plan(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SD_OK : hip_fail(e);
 }
 

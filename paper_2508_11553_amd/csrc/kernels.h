@@ -692,6 +692,60 @@ struct EvictArgs {
     int32_t new_pages;                   // of a sequence: ceil(min(budget, max_context_len) / 16)
 };
 
+// Tokens drawn from rows of logits (sample.hip).
+constexpr int kMaxVocab = (1 << 20) - 1;   // whose weights of 43 bits add up in 64
+struct SampleArgs {
+    const void *logits;                  // row r at r * stride elements
+    int64_t stride;
+    int32_t rows, vocab;
+    const float *temperature;            // [rows] each, or null
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    const float *uniform;                // [rows]
+    int32_t *tokens;                     // [rows]
+    float *logprobs, *draw_logprobs;     // [rows] or null
+};
+
+// Log probabilities of given tokens (token_logprobs.hip).
+constexpr int kGradVectors = 4;          // 16-byte vectors of a thread of the gradient
+struct LogprobArgs {
+    const void *logits;
+    int64_t stride;
+    int32_t rows, vocab;
+    const int32_t *targets;              // [rows]; outside [0, vocab): padding
+    const float *temperature;            // [rows] or null
+    float *logprobs, *entropy, *stats;   // [rows], [rows] or null, [rows][2] or null
+    float *parts;                        // [rows][slices][3], slices > 1
+    int32_t slices;                      // workgroups of a row
+    Division per_row;                    // by slices
+};
+struct LogprobGradArgs {
+    const void *logits;
+    int64_t stride;
+    int32_t rows, vocab;
+    const int32_t *targets;
+    const float *temperature, *stats, *entropy, *d_logprobs, *d_entropy;
+    void *d_logits;                      // laid out as logits
+    int32_t slices;
+    Division per_row;
+};
+
+// Places of new tokens (plan_step.hip).
+struct PlanArgs {
+    const int32_t *new_tokens, *shared_len;       // [B]; the latter may be null
+    const int32_t *lens_in, *next_in, *free_in;   // [B], [B] or null, [1]
+    int32_t *lens_out, *next_out, *free_out;
+    int32_t *free_pages;                          // [num_pages], a stack
+    int32_t *block_table;
+    int32_t *granted, *row_start, *starts;        // [B], [B + 1], [B]
+    int32_t *seq_ids, *slots, *positions;         // [max_rows]; positions may be null
+    int64_t *back_from;                           // [B + 1]: pages that sequences before this one give back
+    int32_t *page_from;                           // [B + 1]: pages that sequences before this one take
+    int32_t *next_at;                             // [B]: next_in, which next_out may overwrite
+    int32_t *counts;                              // free_in
+    int32_t B, max_blocks, num_pages, max_context_len, max_rows;
+};
+
 // Launchers: enqueue on `stream`, return the hipError_t of the launch.  When
 // `start`/`stop` are given they are bound to the kernel's own begin and end
 // timestamps (hipExtLaunchKernelGGL), so their elapsed time is the kernel's
@@ -710,6 +764,10 @@ hipError_t launch_norm_rope(const NormRopeArgs &n, const RowPages *pages, int he
 hipError_t launch_norm_rope_backward(const NormRopeArgs &n, const NormGradArgs &d, int k_blocks, int head_dim, hipStream_t stream);
 hipError_t launch_weights(const WeightArgs &a, int pack, int head_dim, int kv_dtype, hipStream_t stream);
 hipError_t launch_evict(const EvictArgs &a, int head_dim, int kv_dtype, hipStream_t stream);
+hipError_t launch_sample(const SampleArgs &a, bool f32, hipStream_t stream);
+hipError_t launch_logprobs(const LogprobArgs &a, bool f32, hipStream_t stream);
+hipError_t launch_logprobs_backward(const LogprobGradArgs &a, bool f32, hipStream_t stream);
+hipError_t launch_plan(const PlanArgs &a, hipStream_t stream);
 hipError_t launch_append(const AppendArgs &a, int head_dim, hipStream_t stream);
 hipError_t launch_append_fp8(const AppendFp8Args &a, int head_dim, hipStream_t stream);
 hipError_t launch_copy_pages(const CopyPagesArgs &a, hipStream_t stream);

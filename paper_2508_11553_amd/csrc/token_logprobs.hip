@@ -1,0 +1,172 @@
+// Log probabilities of given tokens with the entropy of every row, and their gradient.
+//
+//   z = x / temperature,  S = sum exp(z - max z),  log p = z - max z - log S
+//   out: log p of the target,  H = -sum p log p = log S - sum exp(z - max z) (z - max z) / S
+//   gradient, with g that of the log probability and h that of the entropy:
+//   dx_j = (g ([j = target] - p_j) - h p_j (log p_j + H)) / temperature
+//
+// One pass over the logits for the first, one pass that reads and writes for the second: bound by memory.  A lane holds the largest
+// logit so far and the two sums relative to it; where a larger one comes both sums are moved to it.  fp32, joined in 64 bits.
+#include "logits.h"
+
+namespace sd {
+
+namespace {
+
+constexpr int kLogprobThreads = 512, kLogprobWaves = kLogprobThreads / 64;
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kFar = -1e5f;   // 2^kFar is 0, and 0 times it too, which 0 times -inf is not
+
+// sums relative to m: s = sum 2^((x - m) c), t = sum 2^((x - m) c) (x - m) c
+struct RowSums {
+    float m, s, t;
+};
+SD_DEV RowSums joined(RowSums a, RowSums b, float c)
+{
+    const float m = max_of(a.m, b.m);
+    const float da = max_of((a.m - m) * c, kFar), db = max_of((b.m - m) * c, kFar);
+    const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+    return RowSums{m, a.s * ea + b.s * eb, (a.t + a.s * da) * ea + (b.t + b.s * db) * eb};
+}
+SD_DEV float log2_scale(const float *temperature, int64_t r)   // log2(e) / temperature
+{
+    const float t = temperature ? temperature[r] : 1.f;
+    return (float)(kLog2e / (t > 0.f ? (double)t : 1.0));
+}
+
+template <bool F32>
+SD_DEV void finish(const LogprobArgs &a, int64_t r, RowSums x, float c)
+{
+    const LogitRow<F32> row(a.logits, r, a.stride, a.vocab);
+    const int target = a.targets[r];
+    const float log2_sum = x.s > 0.f || x.s != x.s ? (float)log2((double)x.s) : -__builtin_inff();
+    const bool nothing = log2_sum == -__builtin_inff();   // every logit is -inf
+    const float z = (row.at(target) - x.m) * c;
+    a.logprobs[r] = nothing ? log2_sum : (float)(((double)z - log2_sum) * kLn2);
+    if (a.entropy) a.entropy[r] = nothing ? 0.f : (float)((log2_sum - (double)x.t / x.s) * kLn2);
+    // What the gradient needs: the largest logit and log2 of the sum; of a row with nothing a sum past all, which leaves no weight.
+    if (a.stats) a.stats[2 * r] = nothing ? 0.f : x.m, a.stats[2 * r + 1] = nothing ? __builtin_inff() : log2_sum;
+}
+
+}  // namespace
+
+template <bool F32>
+__global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a)
+{
+    using Row = LogitRow<F32>;
+    __shared__ RowSums s_wave[kLogprobWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const unsigned r = a.per_row.of(blockIdx.x), part = blockIdx.x - r * a.slices;
+    const int target = a.targets[r];
+    if ((unsigned)target >= (unsigned)a.vocab) {
+        if (tid == 0 && part == 0) {
+            a.logprobs[r] = 0.f;
+            if (a.entropy) a.entropy[r] = 0.f;
+            if (a.stats) a.stats[2 * r] = a.stats[2 * r + 1] = 0.f;
+        }
+        return;
+    }
+    const Row row(a.logits, r, a.stride, a.vocab);
+    const float c = log2_scale(a.temperature, r);
+    const int per_part = (row.vectors + a.slices - 1) / a.slices;
+    const int end = min(row.vectors, (int)(part + 1) * per_part);
+    RowSums x{kLowest, 0.f, 0.f};
+    for (int v = part * per_part + tid; v < end; v += kLogprobThreads) {
+        const u32x4 w = row.template load<true>(v);
+        float m = x.m;
+#pragma unroll
+        for (int e = 0; e < Row::kEach; ++e) m = max_of(m, Row::value(w, e));
+        const float d = max_of((x.m - m) * c, kFar), scale = __builtin_amdgcn_exp2f(d);
+        x.t = (x.t + x.s * d) * scale;
+        x.s *= scale;
+        x.m = m;
+#pragma unroll
+        for (int e = 0; e < Row::kEach; ++e) {
+            const float z = max_of((Row::value(w, e) - m) * c, kFar), y = __builtin_amdgcn_exp2f(z);
+            x.s += y;
+            x.t += y * z;
+        }
+    }
+    for (int off = 32; off > 0; off /= 2) x = joined(x, RowSums{__shfl_xor(x.m, off, 64), __shfl_xor(x.s, off, 64), __shfl_xor(x.t, off, 64)}, c);
+    if (lane == 0) s_wave[wave] = x;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < kLogprobWaves; ++w) x = joined(x, s_wave[w], c);
+        if (a.slices == 1) finish<F32>(a, r, x, c);
+        else a.parts[3 * (int64_t)blockIdx.x] = x.m, a.parts[3 * (int64_t)blockIdx.x + 1] = x.s, a.parts[3 * (int64_t)blockIdx.x + 2] = x.t;
+    }
+}
+
+// Joins the parts of a row: a wave per row.
+template <bool F32>
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a)
+{
+    const int64_t r = blockIdx.x;
+    if ((unsigned)a.targets[r] >= (unsigned)a.vocab) return;
+    const float c = log2_scale(a.temperature, r);
+    RowSums x{kLowest, 0.f, 0.f};
+    for (int i = threadIdx.x; i < a.slices; i += 64) {
+        const float *p = a.parts + 3 * (r * a.slices + i);
+        x = joined(x, RowSums{p[0], p[1], p[2]}, c);
+    }
+    for (int off = 32; off > 0; off /= 2) x = joined(x, RowSums{__shfl_xor(x.m, off, 64), __shfl_xor(x.s, off, 64), __shfl_xor(x.t, off, 64)}, c);
+    if (threadIdx.x == 0) finish<F32>(a, r, x, c);
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a)
+{
+    using Row = LogitRow<F32>;
+    const unsigned r = a.per_row.of(blockIdx.x), part = blockIdx.x - r * a.slices;
+    const int target = a.targets[r];
+    const bool padding = (unsigned)target >= (unsigned)a.vocab;
+    const Row row(a.logits, r, a.stride, a.vocab);
+    const LogitRow<F32> out(a.d_logits, r, a.stride, a.vocab);
+    const float c = log2_scale(a.temperature, r), inverse = c * (float)kLn2;
+    const float m = a.stats[2 * (int64_t)r], log2_sum = a.stats[2 * (int64_t)r + 1];
+    const float g = padding ? 0.f : a.d_logprobs[r] * inverse, h = padding || !a.d_entropy ? 0.f : a.d_entropy[r] * inverse;
+    const float of_h = a.d_entropy && !padding ? a.entropy[r] : 0.f;
+    const float base = g + h * of_h, slope = h * (float)kLn2, at_target = log2_sum == __builtin_inff() ? 0.f : g;
+    const int per_part = kGradVectors * 256;
+    const int end = min(row.vectors, (int)(part + 1) * per_part);
+    for (int v = part * per_part + threadIdx.x; v < end; v += 256) {
+        float y[Row::kEach];
+        if (padding) {
+#pragma unroll
+            for (int e = 0; e < Row::kEach; ++e) y[e] = 0.f;
+        } else {
+            const u32x4 w = row.template load<true>(v);
+#pragma unroll
+            for (int e = 0; e < Row::kEach; ++e) {
+                const float z = max_of((Row::value(w, e) - m) * c - log2_sum, kFar), q = __builtin_amdgcn_exp2f(z);   // log2 p, p
+                y[e] = -q * (base + slope * z) + (row.index(v, e) == target ? at_target : 0.f);
+            }
+        }
+        u32x4 to;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = F32 ? __builtin_bit_cast(unsigned, y[i]) : cvt_pk_bf16(y[F32 ? 0 : 2 * i], y[F32 ? 0 : 2 * i + 1]);
+        out.store(v, to);
+    }
+}
+
+hipError_t launch_logprobs(const LogprobArgs &a, bool f32, hipStream_t stream)
+{
+    const dim3 grid((unsigned)a.rows * (unsigned)a.slices), rows((unsigned)a.rows);
+    if (f32) hipLaunchKernelGGL(logprob_kernel<true>, grid, dim3(kLogprobThreads), 0, stream, a);
+    else hipLaunchKernelGGL(logprob_kernel<false>, grid, dim3(kLogprobThreads), 0, stream, a);
+    if (a.slices > 1) {
+        if (f32) hipLaunchKernelGGL(logprob_join_kernel<true>, rows, dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL(logprob_join_kernel<false>, rows, dim3(64), 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_logprobs_backward(const LogprobGradArgs &a, bool f32, hipStream_t stream)
+{
+    const dim3 grid((unsigned)a.rows * (unsigned)a.slices);
+    if (f32) hipLaunchKernelGGL(logprob_backward_kernel<true>, grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(logprob_backward_kernel<false>, grid, dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace sd
