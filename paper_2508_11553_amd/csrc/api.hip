@@ -858,11 +858,29 @@ int check_logits(const sd_logits *s, int32_t max_vocab)
     return SD_OK;
 }
 
-// 16-byte vectors that a row reaches into, at most.
+// 16-byte vectors of a row.
 int64_t row_vectors(const sd_logits *s)
 {
     const int each = s->dtype == SD_F32 ? 4 : 8;
-    return ((int64_t)s->vocab + 2 * each - 2) / each;
+    return ((int64_t)s->vocab + each - 1) / each;
+}
+
+constexpr int64_t kSampleWavesAtOnce = 4096;
+
+struct SampleLayout {
+    int32_t stretches;
+    size_t max_off, group_off, total;
+};
+SampleLayout sample_layout(const sd_logits *s)
+{
+    const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    SampleLayout w;
+    w.stretches = (s->vocab + sd::kStretch - 1) / sd::kStretch;
+    const size_t all = (size_t)s->rows * w.stretches;
+    w.max_off = up(all * 8);
+    w.group_off = w.max_off + up(all * 4);
+    w.total = std::max<size_t>(256, w.group_off + all * 64 * (s->dtype == SD_F32 ? 4 : 2));
+    return w;
 }
 
 // No heads and no rows of the pools enter.
@@ -1097,7 +1115,8 @@ int kv_evict(const sd_shape *shape, int32_t budget, int32_t sinks, int32_t recen
 
 size_t sample_workspace_bytes(const sd_logits *shape)
 {
-    return check_logits(shape, sd::kMaxVocab) ? 0 : 256;
+    if (check_logits(shape, sd::kMaxVocab)) return 0;
+    return sample_layout(shape).total;
 }
 
 int sample_tokens(const sd_logits *shape, const void *logits, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
@@ -1109,8 +1128,11 @@ int sample_tokens(const sd_logits *shape, const void *logits, const float *tempe
     if (bad_ptr(logits) || bad_ptr(uniform) || bad_ptr(tokens) || bad_ptr(workspace) || !aligned16(temperature) || !aligned16(top_k) || !aligned16(top_p) ||
         !aligned16(min_p) || !aligned16(logprobs) || !aligned16(draw_logprobs))
         return SD_EINVAL;
-    if (too_many_threads(shape->rows, 1024)) return SD_EUNSUPPORTED;
-    if (workspace_bytes < sample_workspace_bytes(shape)) return SD_EWORKSPACE;
+    const SampleLayout w = sample_layout(shape);
+    const uint64_t waves = (uint64_t)shape->rows * w.stretches;
+    if (waves > 0x7fffffff || too_many_threads(shape->rows, 512) || too_many_threads((waves + 3) / 4, 256)) return SD_EUNSUPPORTED;
+    if (workspace_bytes < w.total) return SD_EWORKSPACE;
+    char *ws = static_cast<char *>(workspace);
     sd::SampleArgs a;
     a.logits = logits;
     a.stride = shape->stride ? shape->stride : shape->vocab;
@@ -1124,6 +1146,14 @@ int sample_tokens(const sd_logits *shape, const void *logits, const float *tempe
     a.tokens = tokens;
     a.logprobs = logprobs;
     a.draw_logprobs = draw_logprobs;
+    a.sums = reinterpret_cast<uint64_t *>(ws);
+    a.maxima = reinterpret_cast<float *>(ws + w.max_off);
+    a.group_maxima = ws + w.group_off;
+    a.stretches = w.stretches;
+    // Stretches of a wave: one, until there are more waves than the machine runs at once
+    a.run = (int32_t)std::min<int64_t>(w.stretches, std::max<int64_t>(1, ((int64_t)waves + kSampleWavesAtOnce - 1) / kSampleWavesAtOnce));
+    a.runs = (w.stretches + a.run - 1) / a.run;
+    a.per_row = sd::division_by(a.runs);
     const hipError_t e = sd::launch_sample(a, shape->dtype == SD_F32, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SD_OK : hip_fail(e);
 }

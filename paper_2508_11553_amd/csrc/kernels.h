@@ -694,6 +694,7 @@ struct EvictArgs {
 
 // Tokens drawn from rows of logits (sample.hip).
 constexpr int kMaxVocab = (1 << 20) - 1;   // whose weights of 43 bits add up in 64
+constexpr int kStretch = 2048;             // logits of a stretch
 struct SampleArgs {
     const void *logits;                  // row r at r * stride elements
     int64_t stride;
@@ -704,6 +705,11 @@ struct SampleArgs {
     const float *uniform;                // [rows]
     int32_t *tokens;                     // [rows]
     float *logprobs, *draw_logprobs;     // [rows] or null
+    uint64_t *sums;                      // [rows][stretches]: whole weights relative to the stretch's largest logit
+    float *maxima;                       // [rows][stretches]
+    void *group_maxima;                  // [rows][stretches][64], the logits' type: of the logits that a lane held
+    int32_t stretches, run, runs;        // of a row; of a wave; waves of a row
+    Division per_row;                    // by runs
 };
 
 // Log probabilities of given tokens (token_logprobs.hip).

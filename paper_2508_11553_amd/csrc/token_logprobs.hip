@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a
 #pragma unroll
             for (int e = 0; e < Row::kEach; ++e) {
                 const float z = max_of((Row::value(w, e) - m) * c - log2_sum, kFar), q = __builtin_amdgcn_exp2f(z);   // log2 p, p
-                y[e] = -q * (base + slope * z) + (row.index(v, e) == target ? at_target : 0.f);
+                y[e] = -q * (base + slope * z) + (v * Row::kEach + e == target ? at_target : 0.f);
             }
         }
         u32x4 to;
