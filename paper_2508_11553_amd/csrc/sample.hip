@@ -17,6 +17,8 @@
 // Where that list would be too long (nearly even logits) the workgroup goes over the row instead.
 #include "logits.h"
 
+#include <type_traits>
+
 namespace sd {
 
 namespace {
@@ -45,21 +47,35 @@ SD_DEV double exp2_of(double t)
     p = __builtin_fma(p, f, 0.2402265069581371);
     p = __builtin_fma(p, f, 0.6931471805585505);
     p = __builtin_fma(p, f, 1.0);
-    const uint64_t bits = __builtin_bit_cast(uint64_t, p);
-    const unsigned exponent = (unsigned)__builtin_bit_cast(uint64_t, y) << 20;
-    return __builtin_bit_cast(double, (uint64_t)((unsigned)(bits >> 32) + exponent) << 32 | (unsigned)bits);
+    return __builtin_amdgcn_ldexp(p, (int)(unsigned)__builtin_bit_cast(uint64_t, y));
 }
 constexpr uint64_t kWholeBias = 0x4330000000000000ull;   // of 2^52
-// How logits of a row weigh: relative to `top`, at log2(e) / temperature.
+// How logits of a row weigh: relative to `top`, at log2(e) / temperature.  Where top c is small its rounding is far below that of a weight, and one
+// instruction makes the exponent of two.  Where top is so large that every other number's exponent is below -44 (`lone`; +inf among them), logits
+// are compared with it instead.
 struct Weigher {
-    double top, c;
-    SD_DEV double exponent(float x) const { return ((double)x - top) * c; }
-    SD_DEV double weight(float x) const { return exp2_of<0>(exponent(x)); }
-    SD_DEV uint64_t biased(float x) const { return __builtin_bit_cast(uint64_t, exp2_of<43>(exponent(x)) + 4503599627370496.0); }
-    SD_DEV uint64_t whole(float x) const { return biased(x) - kWholeBias; }
+    double top, c, shift;
+    bool near;
+    SD_DEV Weigher(float top_, double c_) : top(top_), c(c_), shift(-top * c), near(__builtin_fabs(shift) < 256.0) {}
+    template <bool NEAR>
+    SD_DEV double exponent(float x) const
+    {
+        return NEAR ? __builtin_fma((double)x, c, shift) : ((double)x - top) * c;
+    }
+    SD_DEV double weight(float x) const { return exp2_of<0>(exponent<false>(x)); }   // (of the largest exactly 1)
+    template <bool NEAR>
+    SD_DEV uint64_t biased(float x) const
+    {
+        return __builtin_bit_cast(uint64_t, exp2_of<43>(exponent<NEAR>(x)) + 4503599627370496.0);
+    }
+    SD_DEV uint64_t whole(float x) const { return (near ? biased<true>(x) : biased<false>(x)) - kWholeBias; }
 };
-// Logits of a row whose largest is +inf: those alone count, alike.
-SD_DEV float finite(float x, bool infinite) { return !infinite ? x : x == kInf ? 0.f : -kInf; }
+SD_DEV bool is_lone(float top, float temperature) { return __builtin_fabsf(top) >= 1073741824.f * temperature; }   // (neighbours of top differ by 2^-25 of it or more)
+struct Lone {
+    bool on;
+    float top;
+    SD_DEV float operator()(float x) const { return !on ? x : x == top ? 0.f : -kInf; }
+};
 
 // Keys order as logits do: NaN below everything, the two zeros equal.  Those of bf16 have 16 bits.
 template <bool F32>
@@ -86,6 +102,7 @@ struct RowLimits {
         temperature = a.temperature ? a.temperature[r] : 1.f;
         greedy = !(temperature > 0.f);
         if (greedy) temperature = 1.f;
+        temperature = min(temperature, 0x1p100f);   // no logits differ by so much, and those that are less apart weigh alike
         c = kLog2e / (double)temperature;
         top_k = a.top_k ? a.top_k[r] : 0;
         top_p = a.top_p ? a.top_p[r] : 1.f;
@@ -110,33 +127,49 @@ SD_DEV double stretch_scale(float m, float top, double c)
 }
 SD_DEV double wave_scan_f64(double x)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const double y = __shfl_up(x, off, 64);
-        x += lane >= off ? y : 0.0;
+#define SD_SCAN_STEP(ctrl, rows)                                                                                                    \
+    {                                                                                                                               \
+        const uint64_t u = __builtin_bit_cast(uint64_t, x);                                                                         \
+        const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, rows, 0xf, false);                               \
+        const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, rows, 0xf, false);                       \
+        x += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);                                                                   \
     }
+    SD_SCAN_STEP(0x111, 0xf) SD_SCAN_STEP(0x112, 0xf) SD_SCAN_STEP(0x114, 0xf) SD_SCAN_STEP(0x118, 0xf)
+    SD_SCAN_STEP(0x142, 0xa) SD_SCAN_STEP(0x143, 0xc)
+#undef SD_SCAN_STEP
     return x;
 }
+SD_DEV uint64_t read_lane(uint64_t x, int lane)
+{
+    return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, lane);
+}
+SD_DEV double read_lane(double x, int lane) { return __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, x), lane)); }
 SD_DEV RowTotal row_total(const SampleArgs &a, int64_t r, double c)
 {
     const int lane = threadIdx.x & 63;
     const float *maxima = a.maxima + r * a.stretches;
     const uint64_t *sums = a.sums + r * a.stretches;
-    RowTotal t{-kInf, 0.0};
-    for (int s0 = 0; s0 < a.stretches; s0 += 64) t.top = max_of(t.top, wave_max_of(s0 + lane < a.stretches ? maxima[s0 + lane] : -kInf));
-    for (int s0 = 0; s0 < a.stretches; s0 += 64) {
+    const float first = lane < a.stretches ? maxima[lane] : -kInf;
+    const uint64_t first_sum = lane < a.stretches ? sums[lane] : 0;
+    RowTotal t{wave_max_of(first), 0.0};
+    for (int s0 = 64; s0 < a.stretches; s0 += 64) t.top = max_of(t.top, wave_max_of(s0 + lane < a.stretches ? maxima[s0 + lane] : -kInf));
+    t.sum = read_lane(wave_scan_f64((double)first_sum * stretch_scale(first, t.top, c)), 63);
+    for (int s0 = 64; s0 < a.stretches; s0 += 64) {
         double x = 0.0;
         if (s0 + lane < a.stretches) x = (double)sums[s0 + lane] * stretch_scale(maxima[s0 + lane], t.top, c);
-        t.sum += __shfl(wave_scan_f64(x), 63, 64);
+        t.sum += read_lane(wave_scan_f64(x), 63);
     }
     t.sum *= 1.0 / kOne;
     return t;
 }
 
+struct Drawn {
+    int token;
+    float x;
+};
 // The token of stretch s at which the kept weights' sum reaches `target` (no more than all of them), by one wave.
 template <bool F32, typename W>
-SD_DEV int walk(const LogitRow<F32> &row, int s, uint64_t target, W &&weight)
+SD_DEV Drawn walk(const LogitRow<F32> &row, int s, uint64_t target, W &&weight)
 {
     using Row = LogitRow<F32>;
     constexpr int kLoads = kStretch / 64 / Row::kEach;
@@ -145,7 +178,7 @@ SD_DEV int walk(const LogitRow<F32> &row, int s, uint64_t target, W &&weight)
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) w[j] = row.load(s * (kStretch / Row::kEach) + j * 64 + lane);
     uint64_t before = 0;
-    int token = -1;
+    Drawn d{-1, 0.f};
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
         const int first = s * kStretch + (j * 64 + lane) * Row::kEach;
@@ -160,29 +193,31 @@ SD_DEV int walk(const LogitRow<F32> &row, int s, uint64_t target, W &&weight)
         if (here) {   // (wave-uniform)
             uint64_t x = ends - sum;
             int e0 = 0;
+            float value = 0.f;
 #pragma unroll
             for (int e = 0; e < Row::kEach; ++e) {
-                if (x < target && x + mine[e] >= target) e0 = e;
+                if (x < target && x + mine[e] >= target) e0 = e, value = Row::value(w[j], e);
                 x += mine[e];
             }
-            token = __builtin_amdgcn_readlane(first + e0, (int)__builtin_ctzll(here));
+            const int which = (int)__builtin_ctzll(here);
+            d.token = __builtin_amdgcn_readlane(first + e0, which);
+            d.x = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, value), which));
             break;
         }
-        before = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(ends >> 32), 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)ends, 63);
+        before = read_lane(ends, 63);
     }
-    return token;
+    return d;
 }
 
 // kept: the weight that the token was drawn from, relative to the largest.
-template <bool F32>
-SD_DEV void write_token(const SampleArgs &a, int64_t r, const LogitRow<F32> &row, int token, const RowLimits &l, const RowTotal &t, double kept)
+SD_DEV void write_token(const SampleArgs &a, int64_t r, const Drawn &d, const RowLimits &l, const RowTotal &t, double kept)
 {
-    if ((threadIdx.x & 63) != 0) return;
-    a.tokens[r] = token;
-    if (!a.logprobs && !a.draw_logprobs) return;
-    const double z = t.top == kInf ? 0.0 : ((double)row.at(token) - t.top) * (1.0 / (double)l.temperature);
-    if (a.logprobs) a.logprobs[r] = (float)(z - log(t.sum));
-    if (a.draw_logprobs) a.draw_logprobs[r] = l.greedy ? 0.f : (float)(z - log(kept));
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) a.tokens[r] = d.token;
+    float *to = lane == 0 ? a.logprobs : a.draw_logprobs;
+    if (lane > 1 || !to) return;
+    const double z = d.x == t.top ? 0.0 : ((double)d.x - t.top) * (1.0 / (double)l.temperature);
+    to[r] = lane == 1 && l.greedy ? 0.f : (float)(z - log(lane == 0 ? t.sum : kept));
 }
 SD_DEV bool write_nothing(const SampleArgs &a, int64_t r, const RowTotal &t)
 {
@@ -209,14 +244,14 @@ SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l)
         for (int s0 = 0; s0 < a.stretches; s0 += 64) {
             const uint64_t here = __builtin_amdgcn_ballot_w64(s0 + lane < a.stretches && maxima[s0 + lane] == t.top);
             if (!here) continue;
-            const int token = walk<F32>(row, s0 + (int)__builtin_ctzll(here), 1, [&](float x, int) { return (uint64_t)(x == t.top); });
-            write_token(a, r, row, token, l, t, 1.0);
+            write_token(a, r, walk<F32>(row, s0 + (int)__builtin_ctzll(here), 1, [&](float x, int) { return (uint64_t)(x == t.top); }), l, t, 1.0);
             return;
         }
     }
     const double u = a.uniform[r], aim = (u > 0.0 ? u : 0.0) * (t.sum * kOne);
     double before = 0.0;
-    int at = 0;          // the stretch, what it holds and how far into it
+    int at = 0;   // the stretch, its largest logit, how far into it
+    float top = -kInf;
     uint64_t target = 1;
     for (int s0 = 0; s0 < a.stretches; s0 += 64) {
         const bool some = s0 + lane < a.stretches;
@@ -234,16 +269,15 @@ SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l)
                 want = want > sum ? sum : want;
             }
             at = s0 + which;
-            target = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(want >> 32), which) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)want, which);
+            top = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), which));
+            target = read_lane(want, which);
         }
         if (over) break;
-        before = __shfl(ends, 63, 64);
+        before = read_lane(ends, 63);
     }
-    const float m = maxima[at];
-    const bool infinite = m == kInf;
-    const Weigher weigh{infinite ? 0.0 : (double)m, l.c};
-    const int token = walk<F32>(row, at, target, [&](float x, int) { return weigh.whole(finite(x, infinite)); });
-    write_token(a, r, row, token, l, t, t.sum);
+    const Lone lone{is_lone(top, l.temperature), top};
+    const Weigher weigh(lone(top), l.c);
+    write_token(a, r, walk<F32>(row, at, target, [&](float x, int) { return weigh.whole(lone(x)); }), l, t, t.sum);
 }
 
 }  // namespace
@@ -296,17 +330,21 @@ __global__ __launch_bounds__(256) void sample_stretch_kernel(SampleArgs a)
         }
         const float top = wave_max_of(m);
         uint64_t sum = 0;
-        if (top == kInf) {
+        if (is_lone(top, l.temperature)) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j)
 #pragma unroll
-                for (int e = 0; e < Row::kEach; ++e) sum += Row::value(w[j], e) == kInf ? (uint64_t)kOne : 0;
-        } else if (top != -kInf) {
-            const Weigher weigh{(double)top, l.c};
+                for (int e = 0; e < Row::kEach; ++e) sum += Row::value(w[j], e) == top && top != -kInf ? (uint64_t)kOne : 0;
+        } else {
+            const Weigher weigh(top, l.c);
+            auto add = [&](auto near) {
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j)
+                for (int j = 0; j < kLoads; ++j)
 #pragma unroll
-                for (int e = 0; e < Row::kEach; ++e) sum += weigh.biased(Row::value(w[j], e));
+                    for (int e = 0; e < Row::kEach; ++e) sum += weigh.template biased<decltype(near)::value>(Row::value(w[j], e));
+            };
+            if (weigh.near) add(std::true_type());
+            else add(std::false_type());
             sum -= kLoads * Row::kEach * kWholeBias;
         }
         sum = wave_scan64(sum);
@@ -336,9 +374,10 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     using Row = LogitRow<F32>;
     using ull = unsigned long long;
     constexpr int kLoads = kStretch / 64 / Row::kEach, kVectors = kStretch / Row::kEach;   // of a lane, of a stretch
+    constexpr int kHeld = 8;   // lanes' maxima that a thread holds
     __shared__ uint64_t s_bins[kBins], s_list[kList], s_stretch[kMaxStretches + 1], s_wave[kChooseWaves];
     __shared__ int s_groups[kGroups], s_rank[kRanked];
-    __shared__ uint64_t s_found[2];
+    __shared__ uint64_t s_found[2], s_base;
     __shared__ int s_n[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t r = blockIdx.x;
@@ -348,28 +387,51 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         return;
     }
     const Row row(a.logits, r, a.stride, a.vocab);
+    // the lanes' maxima
+    const int groups = a.stretches * 64;
+    auto load_max = [&](int i) {
+        const int64_t at = r * groups + i;
+        return F32 ? static_cast<const float *>(a.group_maxima)[at] : __builtin_bit_cast(float, (unsigned)static_cast<const unsigned short *>(a.group_maxima)[at] << 16);
+    };
+    float held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = i * kChooseThreads + tid < groups ? load_max(i * kChooseThreads + tid) : -kInf;
+    for (int i = tid; i < kBins; i += kChooseThreads) s_bins[i] = 0;
+    for (int i = tid; i < a.stretches; i += kChooseThreads) s_stretch[i] = 0;
+    if (tid < kRanked) s_rank[tid] = 0;
+    if (tid < 2) s_n[tid] = 0, s_found[tid] = kBins;
     const RowTotal total = row_total(a, r, l.c);
     if (total.top == -kInf) {
         if (wave == 0) write_nothing(a, r, total);
         return;
     }
-    const bool infinite = total.top == kInf;
-    const float top = infinite ? 0.f : total.top;
-    const Weigher weigh{(double)top, l.c};
+    const Lone lone{is_lone(total.top, l.temperature), total.top};
+    const float top = lone(total.top);
+    const Weigher weigh(top, l.c);
+    __syncthreads();
+    auto each_max = [&](auto &&use) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) use(i * kChooseThreads + tid, lone(held[i]));
+        for (int i = kHeld * kChooseThreads + tid; i < groups; i += kChooseThreads) use(i, lone(load_max(i)));
+    };
 
-    // Bins of logits, from the largest down, 64 to the power of e; the last one's weights are 0.  (Halves: a difference of the largest floats is none.)
-    const float steps = 2.f * min(64.f / l.temperature, 1e30f), half_top = 0.5f * top;
-    auto bin_of = [&](float x) { return (int)__builtin_fminf((half_top - 0.5f * x) * steps, (float)kFarBin); };
+    // Bins of logits, from the largest down, 64 to the power of e; the last one's weights are 0.
+    float steps = min(64.f / l.temperature, 1e30f);
+    auto bin_of = [&](float x) { return (int)__builtin_fminf((top - x) * steps, (float)kFarBin); };
     int limit = kFarBin - 1;   // the last bin that may hold something that is kept
-    auto lower = [&](double least) { limit = min(limit, (int)__builtin_fmin(-64.0 * log(least) * 1.00001, 1e6) + 1); };   // nothing lighter than `least` is kept
+    auto bins_to = [](double weight) { return __builtin_fmin(-64.0 * log(weight), 1e6); };
+    auto lower = [&](double least) { limit = min(limit, (int)(bins_to(least) * 1.00001) + 1); };   // nothing lighter than `least` is kept
+    float sure = kInf;   // (top - x) up to which a logit is as heavy as min_p without doubt
+    if (l.by_least) sure = (float)(-log((double)l.min_p) * (double)l.temperature * 0.99999);
     if (l.by_least && !(l.by_count && l.by_mass)) lower((double)l.min_p);   // (top_p asks for a share of all that top_k leaves, light ones too)
     // All that are as light as this or lighter hold less than 1 - top_p: they come after.
     if (l.by_mass && !l.by_count) lower((1.0 - (double)l.top_p) * total.sum / (double)a.vocab);
+    auto heavy = [&](float x) { return top - x < sure || weigh.weight(x) >= (double)l.min_p; };
 
     auto clear_bins = [&] {
         __syncthreads();
         for (int i = tid; i < kBins; i += kChooseThreads) s_bins[i] = 0;
-        if (tid == 0) s_found[0] = kBins;
+        if (tid < 2) s_found[tid] = kBins;
         __syncthreads();
     };
     auto add_to_bin = [&](int bin, uint64_t x) { atomicAdd(reinterpret_cast<ull *>(&s_bins[bin]), (ull)x); };
@@ -379,10 +441,10 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         int bin;
         uint64_t before;
     };
-    auto find = [&](uint64_t aim) {
+    auto scan_bins = [&](uint64_t (&x)[kBins / kChooseThreads]) {   // a thread's bins, and the sum before them
         __syncthreads();
         constexpr int kPer = kBins / kChooseThreads;
-        uint64_t x[kPer], sum = 0;
+        uint64_t sum = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) sum += x[i] = s_bins[kPer * tid + i];
         const uint64_t upto = wave_scan64(sum);
@@ -390,6 +452,11 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         __syncthreads();
         uint64_t before = upto - sum;
         for (int w = 0; w < wave; ++w) before += s_wave[w];
+        return before;
+    };
+    auto find = [&](uint64_t aim) {
+        constexpr int kPer = kBins / kChooseThreads;
+        uint64_t x[kPer], before = scan_bins(x);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (before < aim && aim <= before + x[i]) s_found[0] = kPer * tid + i, s_found[1] = before;
@@ -404,36 +471,25 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     };
 
     // What the lanes' maxima say.
-    const int groups = a.stretches * 64;
-    auto group_max = [&](int i) {
-        const int64_t at = r * groups + i;
-        const float x = F32 ? static_cast<const float *>(a.group_maxima)[at] : __builtin_bit_cast(float, (unsigned)static_cast<const unsigned short *>(a.group_maxima)[at] << 16);
-        return finite(x, infinite);
-    };
     if (l.by_count || l.by_mass) {
-        clear_bins();
-        for (int i = tid; i < groups; i += kChooseThreads) {
-            const float x = group_max(i);
+        each_max([&](int, float x) {
             const int bin = bin_of(x);
             if (bin <= limit) add_to_bin(bin, l.by_count ? 1 : weigh.whole(x));
-        }
+        });
         const Found f = find(l.by_count ? (uint64_t)l.top_k : share_of(total.sum * kOne));
         if (f.some) limit = min(limit, f.bin);
     }
     // The lanes that hold something down to the limit, then what they hold: key and index, larger codes come earlier.
-    if (tid < 2) s_n[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < groups; i += kChooseThreads)
-        if (bin_of(group_max(i)) <= limit) {
-            const int n = atomicAdd(&s_n[0], 1);
-            if (n < kGroups) s_groups[n] = i;
-        }
+    each_max([&](int i, float x) {
+        if (bin_of(x) > limit) return;
+        const int n = atomicAdd(&s_n[0], 1);
+        if (n < kGroups) s_groups[n] = i;
+    });
     __syncthreads();
     const int found_groups = s_n[0];
-    auto code_of = [](unsigned key, int i) { return (uint64_t)key << 32 | ~(unsigned)i; };
     auto push = [&](float x, int i) {
         const int n = atomicAdd(&s_n[1], 1);
-        if (n < kList) s_list[n] = code_of(key_of<F32>(x), i);
+        if (n < kList) s_list[n] = (uint64_t)key_of<F32>(x) << 32 | ~(unsigned)i;
     };
     if (found_groups <= kGroups) {
         for (int i = tid; i < found_groups * kLoads; i += kChooseThreads) {
@@ -441,29 +497,103 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
             const u32x4 w = row.load(v);
 #pragma unroll
             for (int e = 0; e < Row::kEach; ++e) {
-                const float x = finite(Row::value(w, e), infinite);
+                const float x = lone(Row::value(w, e));
                 if (bin_of(x) <= limit) push(x, v * Row::kEach + e);
             }
         }
+        __syncthreads();
     }
-    __syncthreads();
     int listed = s_n[1];
     const bool complete = found_groups <= kGroups && listed <= kList;   // the list holds all down to the limit
     bool from_list = complete;
+
+    // Rows that are gone over: by stretches, a wave's vectors of one on their way together.
+    auto each_logit = [&](auto &&use, auto &&ends) {
+        for (int s = wave; s < a.stretches; s += kChooseWaves) {
+            u32x4 w[kLoads];
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) w[j] = row.load(s * kVectors + j * 64 + lane);
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+                for (int e = 0; e < Row::kEach; ++e) use(lone(Row::value(w[j], e)), s * kStretch + (j * 64 + lane) * Row::kEach + e);
+            ends(s);
+        }
+    };
 
     // What is kept: all keys above `bound`, and of those equal to it the indices up to `last`.
     unsigned bound = 0;
     int last = INT_MAX;
     auto kept = [&](unsigned key, int i) { return key > bound || (key == bound && i <= last); };
-    auto heavy = [&](float x) { return !l.by_least || weigh.weight(x) >= (double)l.min_p; };
+    bool summed = false;    // s_stretch holds the weights of what lies in bins before `split`, the list all the others that may be kept
+    int split = 0;
+    uint64_t base = 0;      // the weight of what lies before `split`, light or not
+    auto stays = [&](float x, int i) {
+        const int bin = bin_of(x);
+        return (bin < split || (bin <= limit && kept(key_of<F32>(x), i))) && heavy(x);
+    };
 
-    if (complete && listed <= kRanked && (l.by_count || l.by_mass)) {
+    if (!complete && l.by_mass && !l.by_count) {
+        // The bin in which the share ends, from weights in 32 bits: whole ones of 2^-31 of the row's, each off by less than one and 2^-16 of itself.
+        steps *= (float)(kBins - 2) / (float)(limit + 1);
+        limit = kBins - 2;
+        const float to_exponent = (float)-l.c, whole = (float)(31.0 - log2(total.sum));
+        unsigned *bins = reinterpret_cast<unsigned *>(s_bins);
+        clear_bins();
+        each_logit([&](float x, int) {
+            const float d = top - x;
+            const int bin = (int)__builtin_fminf(d * steps, (float)kFarBin);
+            if (bin <= limit) atomicAdd(&bins[2 * bin], (unsigned)__builtin_amdgcn_exp2f(__builtin_fmaf(d, to_exponent, whole)));
+        }, [](int) {});
+        const double margin = 0x1p31 * (0x1p-15 + (double)a.vocab * 0x1p-31), aim = (double)l.top_p * 0x1p31;
+        constexpr int kPer = kBins / kChooseThreads;
+        uint64_t x[kPer], before = scan_bins(x);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const double starts = (double)before, ends = (double)(before + x[i]);
+            if (starts + margin < aim && ends + margin >= aim) s_found[0] = kPer * tid + i;   // the share ends in no bin before this one
+            if (starts - margin < aim && ends - margin >= aim) s_found[1] = kPer * tid + i;   // nor in one after this one
+            before += x[i];
+        }
+        if (tid == 0) s_n[1] = 0, s_base = 0;
+        __syncthreads();
+        const bool some = s_found[0] < kBins;
+        split = some ? (int)s_found[0] : aim > margin ? kBins - 1 : 0;   // (down to the limit there is less than the share: all of that)
+        limit = min(limit, (int)s_found[1]);
+        // The weights of what lies before, by stretches, and the others into the list.
+        uint64_t sum = 0, all = 0;
+        each_logit([&](float y, int i) {
+            const int bin = bin_of(y);
+            if (bin < split) {
+                const uint64_t w = weigh.whole(y);
+                all += w;
+                if (heavy(y)) sum += w;
+            } else if (bin <= limit) {
+                push(y, i);
+            }
+        }, [&](int s) {
+            sum = wave_scan64(sum);
+            if (lane == 63) s_stretch[s] = sum;
+            sum = 0;
+        });
+        all = wave_scan64(all);
+        if (lane == 63) atomicAdd(reinterpret_cast<ull *>(&s_base), (ull)all);
+        __syncthreads();
+        listed = s_n[1];
+        summed = listed <= kList;
+        if (summed) base = s_base;
+        else split = 0;
+    }
+    auto mass_aim = [&] {   // of what the list holds, or the row
+        const uint64_t aim = share_of(total.sum * kOne);
+        return aim > base ? aim - base : 1;
+    };
+
+    if ((complete || summed) && listed <= kRanked && (l.by_count || l.by_mass)) {
         // Few: each one's rank is counted, the threads of a candidate sharing the others.
         const int width = listed <= 64 ? 64 : listed <= 128 ? 128 : 256, shares = kChooseThreads / width;
         const int i = tid & (width - 1), per = (listed + shares - 1) / shares, j0 = tid / width * per;
         const uint64_t code = i < listed ? s_list[i] : 0;
-        if (tid < kRanked) s_rank[tid] = 0;
-        __syncthreads();
         int rank = 0;
         for (int j = j0; j < min(listed, j0 + per); ++j) rank += s_list[j] > code;
         if (i < listed) atomicAdd(&s_rank[i], rank);
@@ -481,8 +611,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         const uint64_t ends = wave_scan64(sum);
         int n = most;
         if (l.by_mass) {
-            const uint64_t all = __shfl((ull)ends, 63, 64);
-            const uint64_t aim = share_of(l.by_count ? (double)all : total.sum * kOne);
+            const uint64_t aim = l.by_count ? share_of((double)read_lane(ends, 63)) : mass_aim();
             uint64_t upto = ends - sum;
             int before = 0;   // those whose sum does not reach the aim
 #pragma unroll
@@ -492,10 +621,11 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
             }
             n = min(most, 1 + wave_reduce(before, [](int u, int v) { return u + v; }));
         }
-        const uint64_t end_code = s_bins[kRanked + max(0, n - 1)];
-        bound = (unsigned)(end_code >> 32);
-        last = (int)~(unsigned)end_code;
-        __syncthreads();
+        if (n > 0) {
+            const uint64_t end_code = s_bins[kRanked + n - 1];
+            bound = (unsigned)(end_code >> 32);
+            last = (int)~(unsigned)end_code;
+        }
     } else if (l.by_count || l.by_mass) {
         // By histograms, of the list or of the row.
         auto each = [&](auto &&use) {
@@ -505,20 +635,13 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
                     use(key, (int)~(unsigned)s_list[i], value_of<F32>(key));
                 }
             } else {
-                for (int v = tid; v < row.vectors; v += kChooseThreads) {
-                    const u32x4 w = row.load(v);
-#pragma unroll
-                    for (int e = 0; e < Row::kEach; ++e) {
-                        const float x = finite(Row::value(w, e), infinite);
-                        use(key_of<F32>(x), v * Row::kEach + e, x);
-                    }
-                }
+                each_logit([&](float x, int i) { use(key_of<F32>(x), i, x); }, [](int) {});
             }
         };
         for (int by = 0; by < 2; ++by) {   // first the count, then the weight of what it leaves
             const bool mass = by;
             if (mass ? !l.by_mass : !l.by_count) continue;
-            from_list = complete;
+            from_list = complete || summed;
             clear_bins();
             each([&](unsigned key, int i, float x) {
                 const int bin = bin_of(x);
@@ -526,7 +649,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
             });
             uint64_t aim = (uint64_t)l.top_k;
             if (mass) {
-                aim = share_of(total.sum * kOne);
+                aim = mass_aim();
                 if (l.by_count) {   // of what the count left
                     __syncthreads();
                     uint64_t all = 0;
@@ -551,7 +674,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
             constexpr int kLevels = F32 ? 3 : 2;
             uint64_t before = f.before;
             unsigned prefix = 0;
-            int end = INT_MAX;
+            int end = 0;
             for (int level = 0; level < kLevels + 2; ++level) {
                 const bool of_key = level < kLevels;
                 const int bits = of_key ? (F32 ? (level < 2 ? 11 : 10) : (level ? 5 : 11)) : 10;
@@ -573,16 +696,11 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
                 const Found g = find(aim - before);
                 before += g.before;
                 if (of_key) prefix |= (mask - (unsigned)g.bin) << shift;
-                else end = level == kLevels ? g.bin << 10 : end | g.bin;
-                if (level == kLevels - 1) {
-                    if (mass) {   // as many of that weight
-                        const uint64_t one = weigh.whole(value_of<F32>(prefix));
-                        aim = (aim - before + one - 1) / one;
-                        before = 0;
-                    } else {
-                        aim -= before;
-                        before = 0;
-                    }
+                else end |= g.bin << shift;
+                if (level == kLevels - 1) {   // as many of that weight, or of those that are left
+                    const uint64_t one = mass ? weigh.whole(value_of<F32>(prefix)) : 1;
+                    aim = (aim - before + one - 1) / one;
+                    before = 0;
                 }
             }
             bound = prefix;
@@ -591,10 +709,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     }
 
     // The kept weights by stretches.
-    __syncthreads();
-    for (int i = tid; i < a.stretches; i += kChooseThreads) s_stretch[i] = 0;
-    __syncthreads();
-    if (complete) {
+    if (complete || summed) {
         for (int i = tid; i < listed; i += kChooseThreads) {
             const unsigned key = (unsigned)(s_list[i] >> 32);
             const int at = (int)~(unsigned)s_list[i];
@@ -602,44 +717,37 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
             if (kept(key, at) && heavy(x)) atomicAdd(reinterpret_cast<ull *>(&s_stretch[at / kStretch]), (ull)weigh.whole(x));
         }
     } else {
-        for (int s = wave; s < a.stretches; s += kChooseWaves) {
-            uint64_t sum = 0;
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j) {
-                const int v = s * kVectors + j * 64 + lane;
-                const u32x4 w = row.load(v);
-#pragma unroll
-                for (int e = 0; e < Row::kEach; ++e) {
-                    const float x = finite(Row::value(w, e), infinite);
-                    if (bin_of(x) <= limit && kept(key_of<F32>(x), v * Row::kEach + e) && heavy(x)) sum += weigh.whole(x);
-                }
-            }
+        uint64_t sum = 0;
+        each_logit([&](float x, int i) {
+            if (stays(x, i)) sum += weigh.whole(x);
+        }, [&](int s) {
             sum = wave_scan64(sum);
             if (lane == 63) s_stretch[s] = sum;
-        }
+            sum = 0;
+        });
     }
     __syncthreads();
     if (wave != 0) return;
-    uint64_t all = 0;
-    for (int s0 = 0; s0 < a.stretches; s0 += 64) all += s0 + lane < a.stretches ? s_stretch[s0 + lane] : 0;
-    all = wave_reduce((ull)all, [](ull u, ull v) { return u + v; });
+    uint64_t all = lane < a.stretches ? s_stretch[lane] : 0;
+    const uint64_t first = all;
+    for (int s0 = 64; s0 < a.stretches; s0 += 64) all += s0 + lane < a.stretches ? s_stretch[s0 + lane] : 0;
+    all = read_lane(wave_scan64(all), 63);
     const double u = a.uniform[r], aim = u > 0.0 ? u * (double)all : 0.0;
     uint64_t target = aim < (double)all ? (uint64_t)aim + 1 : all, before = 0;
     if (target > all) target = all;
     for (int s0 = 0; s0 < a.stretches; s0 += 64) {
-        const uint64_t x = s0 + lane < a.stretches ? s_stretch[s0 + lane] : 0, ends = before + wave_scan64(x);
+        const uint64_t x = s0 == 0 ? first : s0 + lane < a.stretches ? s_stretch[s0 + lane] : 0, ends = before + wave_scan64(x);
         const uint64_t here = __builtin_amdgcn_ballot_w64(ends >= target);
         if (here) {
             const int which = (int)__builtin_ctzll(here);
-            const uint64_t want = target - __shfl((ull)(ends - x), which, 64);
-            const int token = walk<F32>(row, s0 + which, want, [&](float y, int i) {
-                y = finite(y, infinite);
-                return bin_of(y) <= limit && kept(key_of<F32>(y), i) && heavy(y) ? weigh.whole(y) : 0;
+            const Drawn d = walk<F32>(row, s0 + which, target - read_lane(ends - x, which), [&](float y, int i) {
+                y = lone(y);
+                return stays(y, i) ? weigh.whole(y) : 0;
             });
-            write_token(a, r, row, token, l, total, (double)all * (1.0 / kOne));
+            write_token(a, r, d, l, total, (double)all * (1.0 / kOne));
             return;
         }
-        before = __shfl((ull)ends, 63, 64);
+        before = read_lane(ends, 63);
     }
 }
 
