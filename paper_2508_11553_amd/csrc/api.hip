@@ -865,8 +865,6 @@ int64_t row_vectors(const sd_logits *s)
     return ((int64_t)s->vocab + each - 1) / each;
 }
 
-constexpr int64_t kSampleWavesAtOnce = 4096;
-
 struct SampleLayout {
     int32_t stretches;
     size_t max_off, group_off, total;
@@ -1150,10 +1148,7 @@ int sample_tokens(const sd_logits *shape, const void *logits, const float *tempe
     a.maxima = reinterpret_cast<float *>(ws + w.max_off);
     a.group_maxima = ws + w.group_off;
     a.stretches = w.stretches;
-    // Stretches of a wave: one, until there are more waves than the machine runs at once
-    a.run = (int32_t)std::min<int64_t>(w.stretches, std::max<int64_t>(1, ((int64_t)waves + kSampleWavesAtOnce - 1) / kSampleWavesAtOnce));
-    a.runs = (w.stretches + a.run - 1) / a.run;
-    a.per_row = sd::division_by(a.runs);
+    a.per_row = sd::division_by(a.stretches);
     const hipError_t e = sd::launch_sample(a, shape->dtype == SD_F32, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SD_OK : hip_fail(e);
 }

@@ -708,8 +708,8 @@ struct SampleArgs {
     uint64_t *sums;                      // [rows][stretches]: whole weights relative to the stretch's largest logit
     float *maxima;                       // [rows][stretches]
     void *group_maxima;                  // [rows][stretches][64], the logits' type: of the logits that a lane held
-    int32_t stretches, run, runs;        // of a row; of a wave; waves of a row
-    Division per_row;                    // by runs
+    int32_t stretches;                   // of a row
+    Division per_row;                    // by stretches
 };
 
 // Log probabilities of given tokens (token_logprobs.hip).

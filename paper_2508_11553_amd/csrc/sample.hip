@@ -25,48 +25,65 @@ namespace {
 
 constexpr int kChooseThreads = 512, kChooseWaves = kChooseThreads / 64;
 constexpr int kBins = 2048, kList = 2048, kGroups = 1024, kRanked = 256;
+constexpr int kPowers = 256;
 constexpr int kFarBin = kBins - 1;   // logits whose weight is 0
 constexpr int kMaxStretches = (kMaxVocab + kStretch - 1) / kStretch;
 constexpr double kOne = 8796093022208.0;   // 2^43
 constexpr float kInf = __builtin_inff();
 
-// 2^t 2^BITS for t in [-60, 0], t below and NaN taken as -60.  A polynomial on [-1/2, 1/2] of the smallest relative error (2^-43.5) that is 1 at 0.
-template <int BITS>
+constexpr double kRound = 6755399441055744.0;   // 1.5 2^52: a sum's low bits are what is added to it, rounded
+
+// 2^t for t in [-60, 1), t below and NaN taken as -60.  A polynomial on [-1/2, 1/2] of the smallest relative error (2^-51) that is 1 at 0.
 SD_DEV double exp2_of(double t)
 {
-    constexpr double kRound = 6755399441055744.0 + BITS;   // 1.5 2^52: the sum's low bits are t + BITS, rounded
     t = __builtin_fmax(t, -60.0);
     const double y = t + kRound, f = t - (y - kRound);
-    double p = 9.168123000972248e-08;
-    p = __builtin_fma(p, f, 1.3255182740764668e-06);
-    p = __builtin_fma(p, f, 1.5258493043374333e-05);
-    p = __builtin_fma(p, f, 0.00015403456036911954);
-    p = __builtin_fma(p, f, 0.0013333547331502897);
-    p = __builtin_fma(p, f, 0.00961812915917182);
-    p = __builtin_fma(p, f, 0.05550410873971191);
-    p = __builtin_fma(p, f, 0.2402265069581371);
-    p = __builtin_fma(p, f, 0.6931471805585505);
+    double p = 7.072585949269223e-09;
+    p = __builtin_fma(p, f, 1.0208690299958306e-07);
+    p = __builtin_fma(p, f, 1.321544258792169e-06);
+    p = __builtin_fma(p, f, 1.5252657260200837e-05);
+    p = __builtin_fma(p, f, 0.0001540353044173605);
+    p = __builtin_fma(p, f, 0.0013333558230164974);
+    p = __builtin_fma(p, f, 0.009618129107606888);
+    p = __builtin_fma(p, f, 0.05550410866444772);
+    p = __builtin_fma(p, f, 0.24022650695910097);
+    p = __builtin_fma(p, f, 0.69314718055995);
     p = __builtin_fma(p, f, 1.0);
     return __builtin_amdgcn_ldexp(p, (int)(unsigned)__builtin_bit_cast(uint64_t, y));
 }
+// powers[j] = 2^(j / 256), in LDS: written by the first `threads` threads.
+SD_DEV void make_powers(double *powers, int threads)
+{
+    for (int j = threadIdx.x; j < kPowers; j += threads) powers[j] = exp2_of(j * (1.0 / kPowers));
+}
 constexpr uint64_t kWholeBias = 0x4330000000000000ull;   // of 2^52
-// How logits of a row weigh: relative to `top`, at log2(e) / temperature.  Where top c is small its rounding is far below that of a weight, and one
+// How logits of a row weigh: relative to `top`, at log2(e) / temperature.  In 256ths of an octave: w = 2^(N / 256) 2^(f / 256) with N whole and |f| <= 1/2, the
+// second by a polynomial that is 1 at 0 (relative error 2^-45).  Where top c is small its rounding is far below that of a weight, and one
 // instruction makes the exponent of two.  Where top is so large that every other number's exponent is below -44 (`lone`; +inf among them), logits
 // are compared with it instead.
 struct Weigher {
     double top, c, shift;
+    const double *powers;
     bool near;
-    SD_DEV Weigher(float top_, double c_) : top(top_), c(c_), shift(-top * c), near(__builtin_fabs(shift) < 256.0) {}
-    template <bool NEAR>
-    SD_DEV double exponent(float x) const
+    SD_DEV Weigher(float top_, double c_, const double *powers_)
+        : top(top_), c(c_ * kPowers), shift(-top * c), powers(powers_), near(__builtin_fabs(shift) < 256.0 * kPowers)
     {
-        return NEAR ? __builtin_fma((double)x, c, shift) : ((double)x - top) * c;
     }
-    SD_DEV double weight(float x) const { return exp2_of<0>(exponent<false>(x)); }   // (of the largest exactly 1)
+    SD_DEV double weight(float x) const { return exp2_of(((double)x - top) * (c * (1.0 / kPowers))); }   // (of the largest exactly 1)
+    // w 2^43, rounded, plus kWholeBias
     template <bool NEAR>
     SD_DEV uint64_t biased(float x) const
     {
-        return __builtin_bit_cast(uint64_t, exp2_of<43>(exponent<NEAR>(x)) + 4503599627370496.0);
+        constexpr double kUp = kRound + 43 * kPowers;
+        double t = NEAR ? __builtin_fma((double)x, c, shift) : ((double)x - top) * c;
+        t = __builtin_fmax(t, -60.0 * kPowers);   // (NaN too)
+        const double y = t + kUp, f = t - (y - kUp);
+        const int n = (int)(unsigned)__builtin_bit_cast(uint64_t, y);
+        double p = 3.3083026805413713e-09;
+        p = __builtin_fma(p, f, 3.665566060704036e-06);
+        p = __builtin_fma(p, f, 0.0027076061740622863);
+        p = __builtin_fma(p, f, 1.0);
+        return __builtin_bit_cast(uint64_t, __builtin_fma(p, __builtin_amdgcn_ldexp(powers[n & (kPowers - 1)], n >> 8), 4503599627370496.0));
     }
     SD_DEV uint64_t whole(float x) const { return (near ? biased<true>(x) : biased<false>(x)) - kWholeBias; }
 };
@@ -123,7 +140,7 @@ struct RowTotal {
 SD_DEV double stretch_scale(float m, float top, double c)
 {
     const double t = ((double)m - top) * c;
-    return m == top ? 1.0 : t > -60.0 ? exp2_of<0>(t) : 0.0;
+    return m == top ? 1.0 : t > -60.0 ? exp2_of(t) : 0.0;
 }
 SD_DEV double wave_scan_f64(double x)
 {
@@ -232,7 +249,7 @@ SD_DEV bool write_nothing(const SampleArgs &a, int64_t r, const RowTotal &t)
 
 // A row without limits, or the largest logit, by one wave.
 template <bool F32>
-SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l)
+SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l, const double *powers)
 {
     const int lane = threadIdx.x & 63;
     const LogitRow<F32> row(a.logits, r, a.stride, a.vocab);
@@ -276,86 +293,81 @@ SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l)
         before = read_lane(ends, 63);
     }
     const Lone lone{is_lone(top, l.temperature), top};
-    const Weigher weigh(lone(top), l.c);
+    const Weigher weigh(lone(top), l.c, powers);
     write_token(a, r, walk<F32>(row, at, target, [&](float x, int) { return weigh.whole(lone(x)); }), l, t, t.sum);
 }
 
 }  // namespace
 
-// GROUPS: the lanes' maxima are written too.
+// A wave per stretch.  GROUPS: the lanes' maxima are written too.
 template <bool F32, bool GROUPS>
 __global__ __launch_bounds__(256) void sample_stretch_kernel(SampleArgs a)
 {
     using Row = LogitRow<F32>;
     constexpr int kLoads = kStretch / 64 / Row::kEach;
+    __shared__ double s_powers[kPowers];
     const int lane = threadIdx.x & 63;
     const unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), r = a.per_row.of(item);
-    if (r >= (unsigned)a.rows) return;
-    const Row row(a.logits, r, a.stride, a.vocab);
-    const RowLimits l(a, r);
-    int s = (int)(item - r * a.runs) * a.run;
-    const int end = min(a.stretches, s + a.run);
-    u32x4 w[kLoads], next[kLoads];
-    auto load = [&](u32x4 *to, int at) {
-        if ((at + 1) * kStretch <= a.vocab) {
+    const int s = (int)(item - r * a.stretches);
+    const bool some = r < (unsigned)a.rows;
+    const Row row(a.logits, some ? r : 0, a.stride, a.vocab);
+    u32x4 w[kLoads];
+    if ((s + 1) * kStretch <= a.vocab) {
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) to[j] = *row.vector(at * (kStretch / Row::kEach) + j * 64 + lane);
-        } else {
+        for (int j = 0; j < kLoads; ++j) w[j] = *row.vector(s * (kStretch / Row::kEach) + j * 64 + lane);
+    } else {
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j) to[j] = row.load(at * (kStretch / Row::kEach) + j * 64 + lane);
-        }
-    };
-    if (s < end) load(w, s);
-    for (; s < end; ++s) {
-        if (s + 1 < end) load(next, s + 1);
-        float m = -kInf;
+        for (int j = 0; j < kLoads; ++j) w[j] = row.load(s * (kStretch / Row::kEach) + j * 64 + lane);
+    }
+    const RowLimits l(a, some ? (int)r : 0);
+    make_powers(s_powers, 256);
+    __syncthreads();
+    if (!some) return;
+    float m = -kInf;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int e = 0; e < Row::kEach; e += 2) m = max_of(m, Row::value(w[j], e), Row::value(w[j], e + 1));
+    if (__builtin_amdgcn_ballot_w64(m != m)) {   // NaN becomes -inf
+        m = -kInf;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
 #pragma unroll
-            for (int e = 0; e < Row::kEach; e += 2) m = max_of(m, Row::value(w[j], e), Row::value(w[j], e + 1));
-        if (__builtin_amdgcn_ballot_w64(m != m)) {   // NaN becomes -inf
-            m = -kInf;
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j)
-#pragma unroll
-                for (int e = 0; e < Row::kEach; ++e) {
-                    const float x = Row::value(w[j], e);
-                    if (x != x) {
-                        if (F32) w[j][F32 ? e : 0] = 0xff800000u;
-                        else w[j][F32 ? 0 : e / 2] = e & 1 ? (w[j][F32 ? 0 : e / 2] & 0xffffu) | 0xff800000u : (w[j][F32 ? 0 : e / 2] & 0xffff0000u) | 0xff80u;
-                    } else {
-                        m = max_of(m, x);
-                    }
+            for (int e = 0; e < Row::kEach; ++e) {
+                const float x = Row::value(w[j], e);
+                if (x != x) {
+                    if (F32) w[j][F32 ? e : 0] = 0xff800000u;
+                    else w[j][F32 ? 0 : e / 2] = e & 1 ? (w[j][F32 ? 0 : e / 2] & 0xffffu) | 0xff800000u : (w[j][F32 ? 0 : e / 2] & 0xffff0000u) | 0xff80u;
+                } else {
+                    m = max_of(m, x);
                 }
-        }
-        const float top = wave_max_of(m);
-        uint64_t sum = 0;
-        if (is_lone(top, l.temperature)) {
+            }
+    }
+    const float top = wave_max_of(m);
+    uint64_t sum = 0;
+    if (is_lone(top, l.temperature)) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+            for (int e = 0; e < Row::kEach; ++e) sum += Row::value(w[j], e) == top && top != -kInf ? (uint64_t)kOne : 0;
+    } else {
+        const Weigher weigh(top, l.c, s_powers);
+        auto add = [&](auto near) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j)
 #pragma unroll
-                for (int e = 0; e < Row::kEach; ++e) sum += Row::value(w[j], e) == top && top != -kInf ? (uint64_t)kOne : 0;
-        } else {
-            const Weigher weigh(top, l.c);
-            auto add = [&](auto near) {
-#pragma unroll
-                for (int j = 0; j < kLoads; ++j)
-#pragma unroll
-                    for (int e = 0; e < Row::kEach; ++e) sum += weigh.template biased<decltype(near)::value>(Row::value(w[j], e));
-            };
-            if (weigh.near) add(std::true_type());
-            else add(std::false_type());
-            sum -= kLoads * Row::kEach * kWholeBias;
-        }
-        sum = wave_scan64(sum);
-        const int64_t at = (int64_t)r * a.stretches + s;
-        if (lane == 63) a.sums[at] = sum, a.maxima[at] = top;
-        if (GROUPS) {
-            if (F32) static_cast<float *>(a.group_maxima)[at * 64 + lane] = m;
-            else static_cast<unsigned short *>(a.group_maxima)[at * 64 + lane] = (unsigned short)(__builtin_bit_cast(unsigned, m) >> 16);
-        }
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) w[j] = next[j];
+                for (int e = 0; e < Row::kEach; ++e) sum += weigh.template biased<decltype(near)::value>(Row::value(w[j], e));
+        };
+        if (weigh.near) add(std::true_type());
+        else add(std::false_type());
+        sum -= kLoads * Row::kEach * kWholeBias;
+    }
+    sum = wave_scan64(sum);
+    const int64_t at = (int64_t)r * a.stretches + s;
+    if (lane == 63) a.sums[at] = sum, a.maxima[at] = top;
+    if (GROUPS) {
+        if (F32) static_cast<float *>(a.group_maxima)[at * 64 + lane] = m;
+        else static_cast<unsigned short *>(a.group_maxima)[at * 64 + lane] = (unsigned short)(__builtin_bit_cast(unsigned, m) >> 16);
     }
 }
 
@@ -363,8 +375,12 @@ __global__ __launch_bounds__(256) void sample_stretch_kernel(SampleArgs a)
 template <bool F32>
 __global__ __launch_bounds__(64) void sample_pick_kernel(SampleArgs a)
 {
+    __shared__ double s_powers[kPowers];
     const int r = blockIdx.x;
-    draw_from_all<F32>(a, r, RowLimits(a, r));
+    const RowLimits l(a, r);
+    make_powers(s_powers, 64);
+    __syncthreads();
+    draw_from_all<F32>(a, r, l, s_powers);
 }
 
 // Rows with limits: a workgroup each.
@@ -378,12 +394,16 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     __shared__ uint64_t s_bins[kBins], s_list[kList], s_stretch[kMaxStretches + 1], s_wave[kChooseWaves];
     __shared__ int s_groups[kGroups], s_rank[kRanked];
     __shared__ uint64_t s_found[2], s_base;
+    __shared__ double s_powers[kPowers];
     __shared__ int s_n[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t r = blockIdx.x;
     const RowLimits l(a, (int)r);
     if (!l.by_count && !l.by_mass && !l.by_least) {
-        if (wave == 0) draw_from_all<F32>(a, r, l);
+        if (wave != 0) return;
+        make_powers(s_powers, 64);
+        wave_lds_fence();
+        draw_from_all<F32>(a, r, l, s_powers);
         return;
     }
     const Row row(a.logits, r, a.stride, a.vocab);
@@ -399,6 +419,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     for (int i = tid; i < kBins; i += kChooseThreads) s_bins[i] = 0;
     for (int i = tid; i < a.stretches; i += kChooseThreads) s_stretch[i] = 0;
     if (tid < kRanked) s_rank[tid] = 0;
+    if (tid < kPowers) make_powers(s_powers, kPowers);
     if (tid < 2) s_n[tid] = 0, s_found[tid] = kBins;
     const RowTotal total = row_total(a, r, l.c);
     if (total.top == -kInf) {
@@ -407,7 +428,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     }
     const Lone lone{is_lone(total.top, l.temperature), total.top};
     const float top = lone(total.top);
-    const Weigher weigh(top, l.c);
+    const Weigher weigh(top, l.c, s_powers);
     __syncthreads();
     auto each_max = [&](auto &&use) {
 #pragma unroll
@@ -753,7 +774,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
 
 hipError_t launch_sample(const SampleArgs &a, bool f32, hipStream_t stream)
 {
-    const dim3 rows((unsigned)a.rows), runs((unsigned)(((int64_t)a.rows * a.runs + 3) / 4));
+    const dim3 rows((unsigned)a.rows), runs((unsigned)(((int64_t)a.rows * a.stretches + 3) / 4));
     const bool limits = a.top_k || a.top_p || a.min_p;
     auto go = [&](auto kernel, dim3 grid, unsigned threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, a); };
     if (f32) {
