@@ -181,47 +181,53 @@ SD_DEV RowTotal row_total(const SampleArgs &a, int64_t r, double c)
 }
 
 struct Drawn {
-    int token;
+    int token;   // < 0: not this wave's
     float x;
 };
-// The token of stretch s at which the kept weights' sum reaches `target` (no more than all of them), by one wave.
-template <bool F32, typename W>
-SD_DEV Drawn walk(const LogitRow<F32> &row, int s, uint64_t target, W &&weight)
+// The token of stretch s at which the kept weights' sum reaches `target` (no more than all of them), by WAVES waves that share the stretch's vectors:
+// the wave whose vectors hold it has it.  s_part: a sum for each of a lane's vectors.
+template <bool F32, int WAVES, typename W>
+SD_DEV Drawn walk(const LogitRow<F32> &row, int s, uint64_t target, uint64_t *s_part, W &&weight)
 {
     using Row = LogitRow<F32>;
-    constexpr int kLoads = kStretch / 64 / Row::kEach;
-    const int lane = threadIdx.x & 63;
-    u32x4 w[kLoads];
+    constexpr int kLoads = kStretch / 64 / Row::kEach, kMine = (kLoads + WAVES - 1) / WAVES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    u32x4 w[kMine];
+    uint64_t upto[kMine];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) w[j] = row.load(s * (kStretch / Row::kEach) + j * 64 + lane);
-    uint64_t before = 0;
+    for (int j = 0; j < kMine; ++j)
+        if (wave * kMine + j < kLoads) w[j] = row.load(s * (kStretch / Row::kEach) + (wave * kMine + j) * 64 + lane);
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+        if (wave * kMine + j >= kLoads) break;
+        uint64_t sum = 0;
+#pragma unroll
+        for (int e = 0; e < Row::kEach; ++e) sum += weight(Row::value(w[j], e), s * kStretch + ((wave * kMine + j) * 64 + lane) * Row::kEach + e);
+        upto[j] = wave_scan64(sum);
+        if (lane == 63) s_part[wave * kMine + j] = upto[j];
+    }
+    __syncthreads();
     Drawn d{-1, 0.f};
+    uint64_t before = 0;
+    for (int j = 0; j < wave * kMine && j < kLoads; ++j) before += s_part[j];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-        const int first = s * kStretch + (j * 64 + lane) * Row::kEach;
-        uint64_t mine[Row::kEach], sum = 0;
-#pragma unroll
-        for (int e = 0; e < Row::kEach; ++e) {
-            mine[e] = weight(Row::value(w[j], e), first + e);
-            sum += mine[e];
-        }
-        const uint64_t ends = before + wave_scan64(sum);
-        const uint64_t here = __builtin_amdgcn_ballot_w64(ends >= target);
-        if (here) {   // (wave-uniform)
-            uint64_t x = ends - sum;
-            int e0 = 0;
-            float value = 0.f;
+    for (int j = 0; j < kMine; ++j) {
+        if (wave * kMine + j >= kLoads) break;
+        const uint64_t all = read_lane(upto[j], 63);
+        if (before < target && target <= before + all) {   // (wave-uniform)
+            const int which = (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto[j] >= target));
+            uint64_t x = before + (which ? read_lane(upto[j], which - 1) : 0);
+            const int first = s * kStretch + ((wave * kMine + j) * 64 + which) * Row::kEach;
+            const u32x4 at = {(unsigned)__builtin_amdgcn_readlane((int)w[j][0], which), (unsigned)__builtin_amdgcn_readlane((int)w[j][1], which),
+                              (unsigned)__builtin_amdgcn_readlane((int)w[j][2], which), (unsigned)__builtin_amdgcn_readlane((int)w[j][3], which)};
 #pragma unroll
             for (int e = 0; e < Row::kEach; ++e) {
-                if (x < target && x + mine[e] >= target) e0 = e, value = Row::value(w[j], e);
-                x += mine[e];
+                const uint64_t mine = weight(Row::value(at, e), first + e);
+                if (x < target && x + mine >= target) d = Drawn{first + e, Row::value(at, e)};
+                x += mine;
             }
-            const int which = (int)__builtin_ctzll(here);
-            d.token = __builtin_amdgcn_readlane(first + e0, which);
-            d.x = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, value), which));
-            break;
         }
-        before = read_lane(ends, 63);
+        before += all;
     }
     return d;
 }
@@ -230,6 +236,7 @@ SD_DEV Drawn walk(const LogitRow<F32> &row, int s, uint64_t target, W &&weight)
 SD_DEV void write_token(const SampleArgs &a, int64_t r, const Drawn &d, const RowLimits &l, const RowTotal &t, double kept)
 {
     const int lane = threadIdx.x & 63;
+    if (d.token < 0) return;
     if (lane == 0) a.tokens[r] = d.token;
     float *to = lane == 0 ? a.logprobs : a.draw_logprobs;
     if (lane > 1 || !to) return;
@@ -239,7 +246,7 @@ SD_DEV void write_token(const SampleArgs &a, int64_t r, const Drawn &d, const Ro
 SD_DEV bool write_nothing(const SampleArgs &a, int64_t r, const RowTotal &t)
 {
     if (t.top != -kInf) return false;
-    if ((threadIdx.x & 63) == 0) {
+    if (threadIdx.x == 0) {
         a.tokens[r] = -1;
         if (a.logprobs) a.logprobs[r] = -kInf;
         if (a.draw_logprobs) a.draw_logprobs[r] = -kInf;
@@ -247,9 +254,9 @@ SD_DEV bool write_nothing(const SampleArgs &a, int64_t r, const RowTotal &t)
     return true;
 }
 
-// A row without limits, or the largest logit, by one wave.
-template <bool F32>
-SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l, const double *powers)
+// A row without limits, or the largest logit, by a workgroup of WAVES waves, each of which finds the stretch for itself.
+template <bool F32, int WAVES>
+SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l, const double *powers, uint64_t *s_part)
 {
     const int lane = threadIdx.x & 63;
     const LogitRow<F32> row(a.logits, r, a.stride, a.vocab);
@@ -261,7 +268,7 @@ SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l, co
         for (int s0 = 0; s0 < a.stretches; s0 += 64) {
             const uint64_t here = __builtin_amdgcn_ballot_w64(s0 + lane < a.stretches && maxima[s0 + lane] == t.top);
             if (!here) continue;
-            write_token(a, r, walk<F32>(row, s0 + (int)__builtin_ctzll(here), 1, [&](float x, int) { return (uint64_t)(x == t.top); }), l, t, 1.0);
+            write_token(a, r, walk<F32, WAVES>(row, s0 + (int)__builtin_ctzll(here), 1, s_part, [&](float x, int) { return (uint64_t)(x == t.top); }), l, t, 1.0);
             return;
         }
     }
@@ -294,7 +301,7 @@ SD_DEV void draw_from_all(const SampleArgs &a, int64_t r, const RowLimits &l, co
     }
     const Lone lone{is_lone(top, l.temperature), top};
     const Weigher weigh(lone(top), l.c, powers);
-    write_token(a, r, walk<F32>(row, at, target, [&](float x, int) { return weigh.whole(lone(x)); }), l, t, t.sum);
+    write_token(a, r, walk<F32, WAVES>(row, at, target, s_part, [&](float x, int) { return weigh.whole(lone(x)); }), l, t, t.sum);
 }
 
 }  // namespace
@@ -371,16 +378,17 @@ __global__ __launch_bounds__(256) void sample_stretch_kernel(SampleArgs a)
     }
 }
 
-// Rows without limits: a wave each.
+// Rows without limits: a workgroup each.
 template <bool F32>
-__global__ __launch_bounds__(64) void sample_pick_kernel(SampleArgs a)
+__global__ __launch_bounds__(256) void sample_pick_kernel(SampleArgs a)
 {
     __shared__ double s_powers[kPowers];
+    __shared__ uint64_t s_part[8];
     const int r = blockIdx.x;
     const RowLimits l(a, r);
-    make_powers(s_powers, 64);
+    make_powers(s_powers, 256);
     __syncthreads();
-    draw_from_all<F32>(a, r, l, s_powers);
+    draw_from_all<F32, 4>(a, r, l, s_powers, s_part);
 }
 
 // Rows with limits: a workgroup each.
@@ -400,40 +408,42 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     const int64_t r = blockIdx.x;
     const RowLimits l(a, (int)r);
     if (!l.by_count && !l.by_mass && !l.by_least) {
-        if (wave != 0) return;
-        make_powers(s_powers, 64);
-        wave_lds_fence();
-        draw_from_all<F32>(a, r, l, s_powers);
+        make_powers(s_powers, kChooseThreads);
+        __syncthreads();
+        draw_from_all<F32, kChooseWaves>(a, r, l, s_powers, s_wave);
         return;
     }
     const Row row(a.logits, r, a.stride, a.vocab);
-    // the lanes' maxima
+    // the lanes' maxima: a thread holds the first kHeld * kChooseThreads
     const int groups = a.stretches * 64;
-    auto load_max = [&](int i) {
-        const int64_t at = r * groups + i;
-        return F32 ? static_cast<const float *>(a.group_maxima)[at] : __builtin_bit_cast(float, (unsigned)static_cast<const unsigned short *>(a.group_maxima)[at] << 16);
-    };
-    float held[kHeld];
+    const char *maxima = static_cast<const char *>(a.group_maxima) + r * groups * Row::kSize;
+    u32x4 held[kHeld / Row::kEach];
+    auto load_maxima = [&](u32x4 *to, int first) {
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) held[i] = i * kChooseThreads + tid < groups ? load_max(i * kChooseThreads + tid) : -kInf;
+        for (int j = 0; j < kHeld / Row::kEach; ++j) to[j] = first + kHeld * tid < groups ? reinterpret_cast<const u32x4 *>(maxima + (int64_t)(first + kHeld * tid) * Row::kSize)[j] : u32x4{};
+    };
+    load_maxima(held, 0);
     for (int i = tid; i < kBins; i += kChooseThreads) s_bins[i] = 0;
     for (int i = tid; i < a.stretches; i += kChooseThreads) s_stretch[i] = 0;
     if (tid < kRanked) s_rank[tid] = 0;
     if (tid < kPowers) make_powers(s_powers, kPowers);
     if (tid < 2) s_n[tid] = 0, s_found[tid] = kBins;
     const RowTotal total = row_total(a, r, l.c);
-    if (total.top == -kInf) {
-        if (wave == 0) write_nothing(a, r, total);
-        return;
-    }
+    if (write_nothing(a, r, total)) return;
     const Lone lone{is_lone(total.top, l.temperature), total.top};
     const float top = lone(total.top);
     const Weigher weigh(top, l.c, s_powers);
     __syncthreads();
     auto each_max = [&](auto &&use) {
+        for (int first = 0; first < groups; first += kHeld * kChooseThreads) {
+            u32x4 w[kHeld / Row::kEach];
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) use(i * kChooseThreads + tid, lone(held[i]));
-        for (int i = kHeld * kChooseThreads + tid; i < groups; i += kChooseThreads) use(i, lone(load_max(i)));
+            for (int j = 0; j < kHeld / Row::kEach; ++j) w[j] = held[j];
+            if (first) load_maxima(w, first);
+            if (first + kHeld * tid < groups)
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i) use(first + kHeld * tid + i, lone(Row::value(w[i / Row::kEach], i % Row::kEach)));
+        }
     };
 
     // Bins of logits, from the largest down, 64 to the power of e; the last one's weights are 0.
@@ -462,12 +472,12 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         int bin;
         uint64_t before;
     };
-    auto scan_bins = [&](uint64_t (&x)[kBins / kChooseThreads]) {   // a thread's bins, and the sum before them
+    auto scan_bins = [&](uint64_t (&x)[kBins / kChooseThreads], auto &&value) {   // a thread's bins, and the sum before them
         __syncthreads();
         constexpr int kPer = kBins / kChooseThreads;
         uint64_t sum = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += x[i] = s_bins[kPer * tid + i];
+        for (int i = 0; i < kPer; ++i) sum += x[i] = value(s_bins[kPer * tid + i]);
         const uint64_t upto = wave_scan64(sum);
         if (lane == 63) s_wave[wave] = upto;
         __syncthreads();
@@ -477,7 +487,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     };
     auto find = [&](uint64_t aim) {
         constexpr int kPer = kBins / kChooseThreads;
-        uint64_t x[kPer], before = scan_bins(x);
+        uint64_t x[kPer], before = scan_bins(x, [](uint64_t one) { return one; });
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (before < aim && aim <= before + x[i]) s_found[0] = kPer * tid + i, s_found[1] = before;
@@ -529,17 +539,21 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
     bool from_list = complete;
 
     // Rows that are gone over: by stretches, a wave's vectors of one on their way together.
-    auto each_logit = [&](auto &&use, auto &&ends) {
+    auto each_vector = [&](auto &&use, auto &&ends) {   // use(vector, index of its first logit)
         for (int s = wave; s < a.stretches; s += kChooseWaves) {
             u32x4 w[kLoads];
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) w[j] = row.load(s * kVectors + j * 64 + lane);
 #pragma unroll
-            for (int j = 0; j < kLoads; ++j)
-#pragma unroll
-                for (int e = 0; e < Row::kEach; ++e) use(lone(Row::value(w[j], e)), s * kStretch + (j * 64 + lane) * Row::kEach + e);
+            for (int j = 0; j < kLoads; ++j) use(w[j], s * kStretch + (j * 64 + lane) * Row::kEach);
             ends(s);
         }
+    };
+    auto each_logit = [&](auto &&use, auto &&ends) {
+        each_vector([&](u32x4 w, int first) {
+#pragma unroll
+            for (int e = 0; e < Row::kEach; ++e) use(lone(Row::value(w, e)), first + e);
+        }, ends);
     };
 
     // What is kept: all keys above `bound`, and of those equal to it the indices up to `last`.
@@ -564,11 +578,12 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         each_logit([&](float x, int) {
             const float d = top - x;
             const int bin = (int)__builtin_fminf(d * steps, (float)kFarBin);
-            if (bin <= limit) atomicAdd(&bins[2 * bin], (unsigned)__builtin_amdgcn_exp2f(__builtin_fmaf(d, to_exponent, whole)));
+            const unsigned w = (unsigned)__builtin_amdgcn_exp2f(__builtin_fmaf(d, to_exponent, whole));
+            if (bin <= limit) atomicAdd(&bins[2 * bin + lane % 2], w);   // (two of each bin: logits crowd)
         }, [](int) {});
         const double margin = 0x1p31 * (0x1p-15 + (double)a.vocab * 0x1p-31), aim = (double)l.top_p * 0x1p31;
         constexpr int kPer = kBins / kChooseThreads;
-        uint64_t x[kPer], before = scan_bins(x);
+        uint64_t x[kPer], before = scan_bins(x, [](uint64_t two) { return (two & 0xffffffffu) + (two >> 32); });
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const double starts = (double)before, ends = (double)(before + x[i]);
@@ -583,20 +598,38 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         limit = min(limit, (int)s_found[1]);
         // The weights of what lies before, by stretches, and the others into the list.
         uint64_t sum = 0, all = 0;
-        each_logit([&](float y, int i) {
-            const int bin = bin_of(y);
-            if (bin < split) {
-                const uint64_t w = weigh.whole(y);
-                all += w;
-                if (heavy(y)) sum += w;
-            } else if (bin <= limit) {
-                push(y, i);
-            }
-        }, [&](int s) {
-            sum = wave_scan64(sum);
-            if (lane == 63) s_stretch[s] = sum;
-            sum = 0;
-        });
+        auto sum_up = [&](auto near) {
+            each_vector([&](u32x4 w, int first) {
+                float x[Row::kEach];
+                bool other = false;   // something is left over, or may be light
+#pragma unroll
+                for (int e = 0; e < Row::kEach; ++e) {
+                    const float y = lone(Row::value(w, e)), d = top - y, bin = d * steps;
+                    x[e] = bin < (float)split ? y : -kInf;
+                    other |= bin < (float)split ? !(d < sure) : bin < (float)(limit + 1);
+                }
+                if (__builtin_amdgcn_ballot_w64(other)) {
+#pragma unroll
+                    for (int e = 0; e < Row::kEach; ++e) {
+                        const float y = lone(Row::value(w, e));
+                        if (x[e] == -kInf) {
+                            if (bin_of(y) <= limit) push(y, first + e);
+                        } else if (!heavy(y)) {
+                            all += weigh.whole(y), x[e] = -kInf;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < Row::kEach; ++e) sum += weigh.template biased<decltype(near)::value>(x[e]);
+            }, [&](int s) {
+                sum = wave_scan64(sum - kLoads * Row::kEach * kWholeBias);
+                if (lane == 63) s_stretch[s] = sum;
+                all += lane == 63 ? sum : 0;
+                sum = 0;
+            });
+        };
+        if (weigh.near) sum_up(std::true_type());
+        else sum_up(std::false_type());
         all = wave_scan64(all);
         if (lane == 63) atomicAdd(reinterpret_cast<ull *>(&s_base), (ull)all);
         __syncthreads();
@@ -748,7 +781,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         });
     }
     __syncthreads();
-    if (wave != 0) return;
+    // by every wave alike, up to the token's own
     uint64_t all = lane < a.stretches ? s_stretch[lane] : 0;
     const uint64_t first = all;
     for (int s0 = 64; s0 < a.stretches; s0 += 64) all += s0 + lane < a.stretches ? s_stretch[s0 + lane] : 0;
@@ -761,7 +794,7 @@ __global__ __launch_bounds__(kChooseThreads) void sample_choose_kernel(SampleArg
         const uint64_t here = __builtin_amdgcn_ballot_w64(ends >= target);
         if (here) {
             const int which = (int)__builtin_ctzll(here);
-            const Drawn d = walk<F32>(row, s0 + which, target - read_lane(ends - x, which), [&](float y, int i) {
+            const Drawn d = walk<F32, kChooseWaves>(row, s0 + which, target - read_lane(ends - x, which), s_wave, [&](float y, int i) {
                 y = lone(y);
                 return stays(y, i) ? weigh.whole(y) : 0;
             });
@@ -779,10 +812,10 @@ hipError_t launch_sample(const SampleArgs &a, bool f32, hipStream_t stream)
     auto go = [&](auto kernel, dim3 grid, unsigned threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, a); };
     if (f32) {
         if (limits) go(sample_stretch_kernel<true, true>, runs, 256), go(sample_choose_kernel<true>, rows, kChooseThreads);
-        else go(sample_stretch_kernel<true, false>, runs, 256), go(sample_pick_kernel<true>, rows, 64);
+        else go(sample_stretch_kernel<true, false>, runs, 256), go(sample_pick_kernel<true>, rows, 256);
     } else {
         if (limits) go(sample_stretch_kernel<false, true>, runs, 256), go(sample_choose_kernel<false>, rows, kChooseThreads);
-        else go(sample_stretch_kernel<false, false>, runs, 256), go(sample_pick_kernel<false>, rows, 64);
+        else go(sample_stretch_kernel<false, false>, runs, 256), go(sample_pick_kernel<false>, rows, 256);
     }
     return hipGetLastError();
 }
