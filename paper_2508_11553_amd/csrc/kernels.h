@@ -737,6 +737,7 @@ struct LogprobGradArgs {
 };
 
 // Places of new tokens (plan_step.hip).
+constexpr int kPlanHeld = 4096;          // sequences whose sums LDS holds
 struct PlanArgs {
     const int32_t *new_tokens, *shared_len;       // [B]; the latter may be null
     const int32_t *lens_in, *next_in, *free_in;   // [B], [B] or null, [1]

@@ -81,6 +81,12 @@ SD_DEV T wave_reduce(T x, F f)
     for (int off = 32; off > 0; off /= 2) x = f(x, __shfl_xor(x, off, 64));
     return x;
 }
+// x of one lane (wave-uniform).
+SD_DEV uint64_t read_lane(uint64_t x, int lane)
+{
+    return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, lane);
+}
+SD_DEV double read_lane(double x, int lane) { return __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, x), lane)); }
 // Sum of x over the lanes up to this one, 64 bits.
 SD_DEV uint64_t wave_scan64(uint64_t x)
 {

@@ -156,11 +156,6 @@ SD_DEV double wave_scan_f64(double x)
 #undef SD_SCAN_STEP
     return x;
 }
-SD_DEV uint64_t read_lane(uint64_t x, int lane)
-{
-    return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, lane);
-}
-SD_DEV double read_lane(double x, int lane) { return __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, x), lane)); }
 SD_DEV RowTotal row_total(const SampleArgs &a, int64_t r, double c)
 {
     const int lane = threadIdx.x & 63;
