@@ -1177,9 +1177,15 @@ int token_logprobs(const sd_logits *shape, const void *logits, const int32_t *ta
     a.entropy = entropy;
     a.stats = stats;
     a.parts = static_cast<float *>(workspace);
-    a.slices = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kLogprobParts / shape->rows, row_vectors(shape) / 1024));
+    // Many rows: a workgroup of four waves each, a few to a compute unit.  Fewer: of sixteen waves, as long as one kernel reads a row sooner than two launches
+    // take; else rows are cut, by 2048 vectors at least.  us, 256 threads : 1024 : rows cut (1024 parts at most):
+    //   17 rows of 8000 vectors 7.6 : 6.4 : 9.0    8 of 16384 15.7 : 11.9 : 9.1    64 of 16384 21 : 13.3 : 10.1    64 of 50000 49 : 21 : 14.7    256 of 16384 24 : 16.4 : 18.4
+    //   600 of 12501 22.9 : 23.8   2048 of 4000 26.9 : 32   8192 of 8192 170 : 190   8192 of 125 22 : 51
+    const int64_t vectors = row_vectors(shape);
+    a.slices = shape->rows > 128 || vectors <= 12288 ? 1 : (int32_t)std::min<int64_t>(kLogprobParts / shape->rows, vectors / 2048);
+    a.threads = shape->rows > 512 || a.slices > 1 ? 256 : 1024;
     a.per_row = sd::division_by(a.slices);
-    if (too_many_threads((uint64_t)a.rows * a.slices, 512)) return SD_EUNSUPPORTED;
+    if (too_many_threads((uint64_t)a.rows * a.slices, 1024)) return SD_EUNSUPPORTED;
     const hipError_t e = sd::launch_logprobs(a, shape->dtype == SD_F32, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SD_OK : hip_fail(e);
 }
@@ -1226,6 +1232,7 @@ int kv_plan_step(const sd_shape *shape, const int32_t *new_tokens, const int32_t
     const int rc = check_plan(shape);
     if (rc) return rc;
     if (max_rows < 0) return SD_EINVAL;
+    if (max_rows > 1 << 30) return SD_EUNSUPPORTED;
     if (shape->batch == 0) return SD_OK;
     if (bad_ptr(new_tokens) || !aligned16(shared_len) || bad_ptr(context_lens_in) || bad_ptr(context_lens_out) || !aligned16(next_in) || !aligned16(next_out) ||
         !next_in != !next_out || bad_ptr(free_pages) || bad_ptr(free_in) || bad_ptr(free_out) || bad_ptr(block_table) || bad_ptr(granted) || bad_ptr(row_start) ||

@@ -722,7 +722,7 @@ struct LogprobArgs {
     const float *temperature;            // [rows] or null
     float *logprobs, *entropy, *stats;   // [rows], [rows] or null, [rows][2] or null
     float *parts;                        // [rows][slices][3], slices > 1
-    int32_t slices;                      // workgroups of a row
+    int32_t slices, threads;             // workgroups of a row, their threads
     Division per_row;                    // by slices
 };
 struct LogprobGradArgs {

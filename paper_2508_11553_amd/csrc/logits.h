@@ -48,11 +48,13 @@ struct LogitRow {
         }
         return u32x4{w[0], w[1], w[2], w[3]};
     }
+    template <bool STREAM = false>
     SD_DEV void store(int v, u32x4 w) const   // of a row that is written
     {
         u32x4_anywhere *to = const_cast<u32x4_anywhere *>(vector(v));
         if (whole(v)) {
-            *to = w;
+            if (STREAM) __builtin_nontemporal_store(w, to);
+            else *to = w;
             return;
         }
 #pragma unroll
@@ -62,6 +64,7 @@ struct LogitRow {
                 else reinterpret_cast<unsigned short *>(to)[e] = (unsigned short)(w[F32 ? 0 : e / 2] >> 16 * (e & 1));
             }
     }
+    SD_DEV static u32x4 nothing() { return F32 ? u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u} : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
     SD_DEV static float value(u32x4 w, int e)
     {
         const unsigned u = w[F32 ? e : e / 2];   // (copied out: a bit cast of a vector's element reads element 0)

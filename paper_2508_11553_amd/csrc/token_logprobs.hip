@@ -13,7 +13,6 @@ namespace sd {
 
 namespace {
 
-constexpr int kLogprobThreads = 512, kLogprobWaves = kLogprobThreads / 64;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kFar = -1e5f;   // 2^kFar is 0, and 0 times it too, which 0 times -inf is not
 
@@ -34,27 +33,32 @@ SD_DEV float log2_scale(const float *temperature, int64_t r)   // log2(e) / temp
     return (float)(kLog2e / (t > 0.f ? (double)t : 1.0));
 }
 
-template <bool F32>
-SD_DEV void finish(const LogprobArgs &a, int64_t r, RowSums x, float c)
+SD_DEV void finish(const LogprobArgs &a, int64_t r, RowSums x, float c, float at_target)
 {
-    const LogitRow<F32> row(a.logits, r, a.stride, a.vocab);
-    const int target = a.targets[r];
     const float log2_sum = x.s > 0.f || x.s != x.s ? (float)log2((double)x.s) : -__builtin_inff();
     const bool nothing = log2_sum == -__builtin_inff();   // every logit is -inf
-    const float z = (row.at(target) - x.m) * c;
+    const float z = (at_target - x.m) * c;
     a.logprobs[r] = nothing ? log2_sum : (float)(((double)z - log2_sum) * kLn2);
     if (a.entropy) a.entropy[r] = nothing ? 0.f : (float)((log2_sum - (double)x.t / x.s) * kLn2);
     // What the gradient needs: the largest logit and log2 of the sum; of a row with nothing a sum past all, which leaves no weight.
     if (a.stats) a.stats[2 * r] = nothing ? 0.f : x.m, a.stats[2 * r + 1] = nothing ? __builtin_inff() : log2_sum;
 }
+template <int LANES>
+SD_DEV RowSums join_lanes(RowSums x, float c)
+{
+#pragma unroll
+    for (int off = LANES / 2; off > 0; off /= 2) x = joined(x, RowSums{__shfl_xor(x.m, off, 64), __shfl_xor(x.s, off, 64), __shfl_xor(x.t, off, 64)}, c);
+    return x;
+}
 
 }  // namespace
 
-template <bool F32>
-__global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a)
+template <bool F32, int THREADS>
+__global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a)
 {
     using Row = LogitRow<F32>;
-    __shared__ RowSums s_wave[kLogprobWaves];
+    constexpr int kWaves = THREADS / 64, kAhead = 4;   // vectors of a lane on their way together
+    __shared__ RowSums s_wave[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const unsigned r = a.per_row.of(blockIdx.x), part = blockIdx.x - r * a.slices;
     const int target = a.targets[r];
@@ -67,34 +71,40 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a)
         return;
     }
     const Row row(a.logits, r, a.stride, a.vocab);
-    const float c = log2_scale(a.temperature, r);
+    const float c = log2_scale(a.temperature, r), at_target = row.at(target);
     const int per_part = (row.vectors + a.slices - 1) / a.slices;
     const int end = min(row.vectors, (int)(part + 1) * per_part);
     RowSums x{kLowest, 0.f, 0.f};
-    for (int v = part * per_part + tid; v < end; v += kLogprobThreads) {
-        const u32x4 w = row.template load<true>(v);
+    for (int v0 = part * per_part + tid; v0 < end; v0 += kAhead * THREADS) {
+        u32x4 w[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) w[j] = v0 + j * THREADS < end ? row.template load<true>(v0 + j * THREADS) : Row::nothing();
         float m = x.m;
 #pragma unroll
-        for (int e = 0; e < Row::kEach; ++e) m = max_of(m, Row::value(w, e));
+        for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+            for (int e = 0; e < Row::kEach; e += 2) m = max_of(m, Row::value(w[j], e), Row::value(w[j], e + 1));
         const float d = max_of((x.m - m) * c, kFar), scale = __builtin_amdgcn_exp2f(d);
         x.t = (x.t + x.s * d) * scale;
         x.s *= scale;
         x.m = m;
 #pragma unroll
-        for (int e = 0; e < Row::kEach; ++e) {
-            const float z = max_of((Row::value(w, e) - m) * c, kFar), y = __builtin_amdgcn_exp2f(z);
-            x.s += y;
-            x.t += y * z;
-        }
+        for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+            for (int e = 0; e < Row::kEach; ++e) {
+                const float z = max_of((Row::value(w[j], e) - m) * c, kFar), y = __builtin_amdgcn_exp2f(z);
+                x.s += y;
+                x.t += y * z;
+            }
     }
-    for (int off = 32; off > 0; off /= 2) x = joined(x, RowSums{__shfl_xor(x.m, off, 64), __shfl_xor(x.s, off, 64), __shfl_xor(x.t, off, 64)}, c);
+    x = join_lanes<64>(x, c);
     if (lane == 0) s_wave[wave] = x;
     __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < kLogprobWaves; ++w) x = joined(x, s_wave[w], c);
-        if (a.slices == 1) finish<F32>(a, r, x, c);
-        else a.parts[3 * (int64_t)blockIdx.x] = x.m, a.parts[3 * (int64_t)blockIdx.x + 1] = x.s, a.parts[3 * (int64_t)blockIdx.x + 2] = x.t;
-    }
+    if (wave != 0) return;
+    x = join_lanes<kWaves>(lane < kWaves ? s_wave[lane] : RowSums{kLowest, 0.f, 0.f}, c);
+    if (lane != 0) return;
+    if (a.slices == 1) finish(a, r, x, c, at_target);
+    else a.parts[3 * (int64_t)blockIdx.x] = x.m, a.parts[3 * (int64_t)blockIdx.x + 1] = x.s, a.parts[3 * (int64_t)blockIdx.x + 2] = x.t;
 }
 
 // Joins the parts of a row: a wave per row.
@@ -102,15 +112,16 @@ template <bool F32>
 __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a)
 {
     const int64_t r = blockIdx.x;
-    if ((unsigned)a.targets[r] >= (unsigned)a.vocab) return;
-    const float c = log2_scale(a.temperature, r);
+    const int target = a.targets[r];
+    if ((unsigned)target >= (unsigned)a.vocab) return;
+    const float c = log2_scale(a.temperature, r), at_target = LogitRow<F32>(a.logits, r, a.stride, a.vocab).at(target);
     RowSums x{kLowest, 0.f, 0.f};
     for (int i = threadIdx.x; i < a.slices; i += 64) {
         const float *p = a.parts + 3 * (r * a.slices + i);
         x = joined(x, RowSums{p[0], p[1], p[2]}, c);
     }
-    for (int off = 32; off > 0; off /= 2) x = joined(x, RowSums{__shfl_xor(x.m, off, 64), __shfl_xor(x.s, off, 64), __shfl_xor(x.t, off, 64)}, c);
-    if (threadIdx.x == 0) finish<F32>(a, r, x, c);
+    x = join_lanes<64>(x, c);
+    if (threadIdx.x == 0) finish(a, r, x, c, at_target);
 }
 
 template <bool F32>
@@ -127,37 +138,38 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a
     const float g = padding ? 0.f : a.d_logprobs[r] * inverse, h = padding || !a.d_entropy ? 0.f : a.d_entropy[r] * inverse;
     const float of_h = a.d_entropy && !padding ? a.entropy[r] : 0.f;
     const float base = g + h * of_h, slope = h * (float)kLn2, at_target = log2_sum == __builtin_inff() ? 0.f : g;
-    const int per_part = kGradVectors * 256;
-    const int end = min(row.vectors, (int)(part + 1) * per_part);
-    for (int v = part * per_part + threadIdx.x; v < end; v += 256) {
+    const int v0 = (int)part * kGradVectors * 256 + (int)threadIdx.x;
+    u32x4 w[kGradVectors];
+    if (!padding) {
+#pragma unroll
+        for (int j = 0; j < kGradVectors; ++j)
+            if (v0 + j * 256 < row.vectors) w[j] = row.template load<true>(v0 + j * 256);
+    }
+#pragma unroll
+    for (int j = 0; j < kGradVectors; ++j) {
+        const int v = v0 + j * 256;
+        if (v >= row.vectors) break;
         float y[Row::kEach];
-        if (padding) {
 #pragma unroll
-            for (int e = 0; e < Row::kEach; ++e) y[e] = 0.f;
-        } else {
-            const u32x4 w = row.template load<true>(v);
-#pragma unroll
-            for (int e = 0; e < Row::kEach; ++e) {
-                const float z = max_of((Row::value(w, e) - m) * c - log2_sum, kFar), q = __builtin_amdgcn_exp2f(z);   // log2 p, p
-                y[e] = -q * (base + slope * z) + (v * Row::kEach + e == target ? at_target : 0.f);
-            }
+        for (int e = 0; e < Row::kEach; ++e) {
+            const float z = max_of((Row::value(w[j], e) - m) * c - log2_sum, kFar), q = __builtin_amdgcn_exp2f(z);   // log2 p, p
+            y[e] = padding ? 0.f : -q * (base + slope * z) + (v * Row::kEach + e == target ? at_target : 0.f);
         }
         u32x4 to;
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i] = F32 ? __builtin_bit_cast(unsigned, y[i]) : cvt_pk_bf16(y[F32 ? 0 : 2 * i], y[F32 ? 0 : 2 * i + 1]);
-        out.store(v, to);
+        out.template store<true>(v, to);
+
     }
 }
 
 hipError_t launch_logprobs(const LogprobArgs &a, bool f32, hipStream_t stream)
 {
     const dim3 grid((unsigned)a.rows * (unsigned)a.slices), rows((unsigned)a.rows);
-    if (f32) hipLaunchKernelGGL(logprob_kernel<true>, grid, dim3(kLogprobThreads), 0, stream, a);
-    else hipLaunchKernelGGL(logprob_kernel<false>, grid, dim3(kLogprobThreads), 0, stream, a);
-    if (a.slices > 1) {
-        if (f32) hipLaunchKernelGGL(logprob_join_kernel<true>, rows, dim3(64), 0, stream, a);
-        else hipLaunchKernelGGL(logprob_join_kernel<false>, rows, dim3(64), 0, stream, a);
-    }
+    auto go = [&](auto kernel, dim3 blocks, int threads) { hipLaunchKernelGGL(kernel, blocks, dim3(threads), 0, stream, a); };
+    if (a.threads == 1024) f32 ? go(logprob_kernel<true, 1024>, grid, 1024) : go(logprob_kernel<false, 1024>, grid, 1024);
+    else f32 ? go(logprob_kernel<true, 256>, grid, 256) : go(logprob_kernel<false, 256>, grid, 256);
+    if (a.slices > 1) f32 ? go(logprob_join_kernel<true>, rows, 64) : go(logprob_join_kernel<false>, rows, 64);
     return hipGetLastError();
 }
 
