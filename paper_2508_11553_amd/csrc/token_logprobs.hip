@@ -27,10 +27,11 @@ SD_DEV RowSums joined(RowSums a, RowSums b, float c)
     const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
     return RowSums{m, a.s * ea + b.s * eb, (a.t + a.s * da) * ea + (b.t + b.s * db) * eb};
 }
-SD_DEV float log2_scale(const float *temperature, int64_t r)   // log2(e) / temperature
+// log2(e) / temperature; finite and not 0, so that it times a difference of 0 is 0 and times one of -inf is -inf.
+SD_DEV float log2_scale(const float *temperature, int64_t r)
 {
     const float t = temperature ? temperature[r] : 1.f;
-    return (float)(kLog2e / (t > 0.f ? (double)t : 1.0));
+    return (float)(kLog2e / (t > 0.f ? __builtin_fmin(__builtin_fmax((double)t, 0x1p-126), 0x1p100) : 1.0));
 }
 
 SD_DEV void finish(const LogprobArgs &a, int64_t r, RowSums x, float c, float at_target)
@@ -85,17 +86,18 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a)
 #pragma unroll
             for (int e = 0; e < Row::kEach; e += 2) m = max_of(m, Row::value(w[j], e), Row::value(w[j], e + 1));
         const float d = max_of((x.m - m) * c, kFar), scale = __builtin_amdgcn_exp2f(d);
-        x.t = (x.t + x.s * d) * scale;
-        x.s *= scale;
-        x.m = m;
+        float s = 0.f, t = 0.f;   // (summed by themselves: errors of 32 terms, not of all that a lane has had)
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
 #pragma unroll
             for (int e = 0; e < Row::kEach; ++e) {
                 const float z = max_of((Row::value(w[j], e) - m) * c, kFar), y = __builtin_amdgcn_exp2f(z);
-                x.s += y;
-                x.t += y * z;
+                s += y;
+                t += y * z;
             }
+        x.t = (x.t + x.s * d) * scale + t;
+        x.s = x.s * scale + s;
+        x.m = m;
     }
     x = join_lanes<64>(x, c);
     if (lane == 0) s_wave[wave] = x;
@@ -159,7 +161,6 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a
 #pragma unroll
         for (int i = 0; i < 4; ++i) to[i] = F32 ? __builtin_bit_cast(unsigned, y[i]) : cvt_pk_bf16(y[F32 ? 0 : 2 * i], y[F32 ? 0 : 2 * i + 1]);
         out.template store<true>(v, to);
-
     }
 }
 

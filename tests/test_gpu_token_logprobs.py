@@ -194,3 +194,26 @@ def test_results_that_are_not_asked_for(sd):  # noqa: F811
     full = forward(b, [1, 2, 3, 4])
     lp, H = forward(b, [1, 2, 3, 4], entropy=False, stats=False)
     assert np.array_equal(lp, full[0]) and (H == 7).all() and (b.stats == 7).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_temperatures_at_the_ends_of_the_range(sd, kind):  # noqa: F811
+    """The smallest leave the largest logits alone, however near the next ones are; the largest weigh all alike that are not masked; 0, below and NaN count as 1."""
+    rng = np.random.default_rng(13)
+    vocab = 1001
+    x = np.tile(rng.normal(0, 2, vocab), (8, 1))
+    x[:, 3::7] = -np.inf
+    x[:, [5, 700]] = 9.0
+    t = [1e-45, 1e-39, 2e-38, np.inf, 3e38, 0.0, -1.0, np.nan]
+    b = Batch(sd, x, kind)
+    targets = [5, 4, 700, 5, 700, 5, 5, 5]
+    lp, H = forward(b, targets, t)
+    some = np.isfinite(b.x[0]).sum()
+    assert abs(lp[0] + np.log(2)) <= 4 * STEP and lp[1] < -1e30 and abs(lp[2] + np.log(2)) <= 4 * STEP and (abs(H[:3] - np.log(2)) <= 8 * STEP).all()
+    assert (abs(lp[3:5] + np.log(some)) <= 16 * STEP * np.log(some)).all() and (abs(H[3:5] - np.log(some)) <= 16 * STEP * np.log(some)).all()
+    assert lp[5] == lp[6] == lp[7] and H[5] == H[6] == H[7]
+    one = forward(Batch(sd, x[5:], kind), targets[5:])
+    assert np.array_equal(one[0], lp[5:]) and np.array_equal(one[1], H[5:])
+    forward(b, targets, t)
+    d = backward(b, [1e-30] * 8, [1e-30] * 8)
+    assert np.isfinite(d).all() and not d[:, ~np.isfinite(b.x[0])].any()
