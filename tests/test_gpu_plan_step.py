@@ -152,3 +152,42 @@ def test_a_batch_of_nothing(sd):
     p = Plan(sd, [7], 4, 1, 8)
     p.shape.batch = 0
     sd.kv_plan_step(p.shape, None, None, None, None, None, None, None, None, None, None, 0, None, None, None, None, None, None, None, 0)
+
+
+@pytest.mark.parametrize("batch", [4095, 4096, 4097, 8191, 12345, 40000])
+def test_batches_that_take_several_turns(sd, batch):
+    """More sequences than one workgroup holds at once, and more than the second kernel keeps sums of."""
+    rng = np.random.default_rng(batch)
+    p = Plan(sd, rng.integers(0, 40, batch), 4, batch // 3, batch)
+    for i in range(2):
+        new = np.where(rng.random(batch) < 0.2, -1, np.where(rng.random(batch) < 0.2, 0, rng.integers(1, 12, batch)))
+        p.step([int(n) for n in new], shared=[int(n) for n in rng.integers(0, 20, batch) // 16 * 16] if i else None, max_rows=[None, batch * 4 + 3][i])
+        if i == 0:
+            pages_once(p)
+
+
+def test_the_last_free_page_and_none_at_all(sd):
+    """Two sequences ask for the one page that is left: the first gets it; with none left only those that need none go on."""
+    p = Plan(sd, [16, 16, 5], 4, 1, 1)
+    assert p.step([1, 1, 1])["granted"] == [1, 0, 0 + 1]
+    assert p.step([1, 1, 1])["granted"] == [1, 0, 1]
+    assert p.step([1, 1, -1])["granted"] == [1, 1, 0]
+    pages_once(p)
+
+
+def test_counts_out_of_range(sd):
+    """A count of free pages below zero counts as none, one above the pool as the pool; entries outside it are only moved, never followed."""
+    import torch
+    for count, granted in ((-5, [0, 1]), (10 ** 9, [1, 1])):
+        p = Plan(sd, [16, 3], 4, 6, 2)
+        d, B = p.d, 2
+        out = {name: torch.zeros(8, dtype=torch.int32, device="cuda") for name in NAMES}
+        new, free_in, free_out = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([1, 1], [count], [0]))
+        sd.kv_plan_step(p.shape, new, None, d["lens"], out["lens_out"], None, None, d["free_pages"], free_in, free_out, d["block_table"], 4, out["granted"], out["row_start"],
+                        out["starts"], out["seq_ids"], out["slots"], out["positions"], d["work"], p.ws)
+        assert out["granted"][:B].tolist() == granted
+        assert free_out.item() == (0 if count < 0 else p.pages - 1)
+    p = Plan(sd, [40, 16], 4, 0, 3)
+    p.d["block_table"][0, :3] = torch.tensor([-7, 2 ** 31 - 1, 1000], dtype=torch.int32, device="cuda")
+    p.table[0][:3] = [-7, 2 ** 31 - 1, 1000]
+    p.step([-1, 17], max_rows=17)
