@@ -687,6 +687,7 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
             s_bins[s_rank[tid]] = weigh.whole(value_of<F32>((unsigned)(code >> 32)));
             s_bins[kRanked + s_rank[tid]] = code;
         }
+        if (tid < kRanked) s_bins[2 * kRanked + tid] = 0;
         __syncthreads();
         // by every wave alike
         uint64_t x[4], sum = 0;
@@ -710,6 +711,32 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
             const uint64_t end_code = s_bins[kRanked + n - 1];
             bound = (unsigned)(end_code >> 32);
             last = (int)~(unsigned)end_code;
+        }
+        if (complete) {
+            // All that is kept is at hand: the weight up to each one, by index, in the same way, and the draw.
+            if (l.by_least) {
+                __syncthreads();
+                if (tid < n && !heavy(value_of<F32>((unsigned)(s_bins[kRanked + tid] >> 32)))) s_bins[tid] = 0;
+                __syncthreads();
+            }
+            const unsigned mine = i < n ? (unsigned)s_bins[kRanked + i] : 0;   // (larger ones are lower indices)
+            uint64_t upto = 0;
+            for (int j = j0; j < min(n, j0 + per); ++j) upto += (unsigned)s_bins[kRanked + j] >= mine ? s_bins[j] : 0;
+            if (i < n) atomicAdd(reinterpret_cast<ull *>(&s_bins[2 * kRanked + i]), (ull)upto);
+            uint64_t all = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) all += 4 * lane + e < n ? s_bins[4 * lane + e] : 0;
+            all = read_lane(wave_scan64(all), 63);
+            const double u = a.uniform[r], aim = u > 0.0 ? u * (double)all : 0.0;
+            const uint64_t target = aim < (double)all ? min((uint64_t)aim + 1, all) : all;
+            __syncthreads();
+            if (tid < n) {
+                const uint64_t end = s_bins[2 * kRanked + tid], one = s_bins[tid];
+                if (end - one < target && target <= end) s_found[0] = s_bins[kRanked + tid];
+            }
+            __syncthreads();
+            if (wave == 0) write_token(a, r, Drawn{(int)~(unsigned)s_found[0], lone.on ? total.top : value_of<F32>((unsigned)(s_found[0] >> 32))}, l, total, (double)all * (1.0 / kOne));
+            return;
         }
     } else if (l.by_count || l.by_mass) {
         // By histograms, of the list or of the row.
