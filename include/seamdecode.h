@@ -527,8 +527,9 @@ typedef struct {
  *     of those the ones with w >= min_p,
  * and draws the first token, by index, for which the weight of the kept tokens up to it
  * exceeds uniform times the weight of all that are kept.  Weights are rounded to multiples of 2^-43
- * and their sums exact: a row's token depends on nothing but the row and its parameters,
- * not on the batch around it, and is the same in every call.
+ * (of the largest weight, in a row without limits that of 2048 tokens), added as whole numbers, and stretches of
+ * 2048 tokens in an order that the row alone fixes: a row's token depends on nothing but the row and
+ * its parameters, not on the batch around it, and is the same in every call.
  *
  *   temperature     f32 [rows] or NULL: 1.  0, negative or NaN: the largest logit is taken, of equal ones
  *                   the first; the log probabilities are those of T = 1 and draw_logprobs 0

@@ -50,43 +50,42 @@ SD_DEV double exp2_of(double t)
     p = __builtin_fma(p, f, 1.0);
     return __builtin_amdgcn_ldexp(p, (int)(unsigned)__builtin_bit_cast(uint64_t, y));
 }
-// powers[j] = 2^(j / 256), its last bit set, less j << 44 (which the exponent's bits bring back, see Weigher), in LDS: by the first `threads` threads.
-SD_DEV void make_powers(u32x2 *powers, int threads)
-{
-    for (int j = threadIdx.x; j < kPowers; j += threads) powers[j] = __builtin_bit_cast(u32x2, (__builtin_bit_cast(uint64_t, exp2_of(j * (1.0 / kPowers))) | 1) - ((uint64_t)j << 44));
-}
 constexpr double kNone = 4503599627370496.0;   // 2^52
 constexpr uint64_t kNoneBits = 0x4330000000000000ull;
-constexpr int kOctaves = 64;
-// How logits of a row weigh: relative to `top`, at log2(e) / temperature.  A logit's position is 1 - (octaves below top) / 64, not below 0 (NaN: 0), which costs
-// nothing: products are clamped to [0, 1] on their way out.  In 256ths of an octave w 2^43 = 2^(n / 256) 2^(f / 256) with n whole and |f| <= 1/2, the second by a
-// polynomial that is 1 at 0 (relative error 2^-45), the first from the table: n << 12 added to the high word makes the exponent of n >> 8 and takes
-// back the j = n & 255 that the table holds too little.  Where top c is small its rounding is far below that of a weight, and one
-// instruction makes the position.
+constexpr int kOctaves = 64;   // below the largest logit; beyond there is no weight
+// powers[j] = 2^(j / 256 - 21), its last bit set, less j << 44 (which the exponent's bits bring back, see Weigher), in LDS: by the first `threads` threads.
+SD_DEV void make_powers(u32x2 *powers, int threads)
+{
+    for (int j = threadIdx.x; j < kPowers; j += threads)
+        powers[j] = __builtin_bit_cast(u32x2, (__builtin_bit_cast(uint64_t, exp2_of(j * (1.0 / kPowers) + (43 - kOctaves))) | 1) - ((uint64_t)j << 44));
+}
+// How logits of a row weigh: relative to `top`, at log2(e) / temperature.  A logit's position is 2^14 less the 256ths of an octave that it lies below top.  Its whole
+// part n (0 for all below 0, -inf and NaN) and the rest f make w 2^43 = 2^(n / 256 - 21) 2^(f / 256), the second by a polynomial (relative error 2^-45.7), the first
+// from the table: n << 12 added to the high word makes the exponent of n >> 8 and takes back the j = n & 255 that the table holds too
+// little.  Where top c is small its rounding is far below that of a weight, and one instruction makes the position.
 // Sums are held above 2^52, where a fused product rounds to whole numbers: each weight by itself, as no weight lies halfway between two (its
 // odd factor from the table has 53 bits, more than a whole number below 2^44 and a half).
 struct Weigher {
-    double top, c, shift, steps, up;
+    double top, c, shift;
     const u32x2 *powers;
     bool near;
     SD_DEV Weigher(float top_, double c_, const u32x2 *powers_)
-        : top(top_), c(c_ * (1.0 / kOctaves)), shift(1.0 - top * c), steps(kOctaves * kPowers), up(kRound + 43.0 * kPowers - kOctaves * kPowers), powers(powers_), near(__builtin_fabs(top * c) < 4.0)
+        : top(top_), c(c_ * kPowers), shift(kOctaves * kPowers - top * c), powers(powers_), near(__builtin_fabs(top * c) < 65536.0)
     {
-        asm("" : "+s"(steps), "+v"(up));   // (kept in registers: an instruction takes one constant)
     }
-    SD_DEV double weight(float x) const { return exp2_of(((double)x - top) * (c * kOctaves)); }   // (of the largest exactly 1)
+    SD_DEV double weight(float x) const { return exp2_of(((double)x - top) * (c * (1.0 / kPowers))); }   // (of the largest exactly 1)
     // sum + w 2^43, rounded; sum is a whole number in [2^52, 2^53)
     template <bool NEAR>
     SD_DEV double add(double sum, float x) const
     {
-        double t = NEAR ? __builtin_fma((double)x, c, shift) : __builtin_fma((double)x - top, c, 1.0);
-        t = __builtin_fmin(__builtin_fmax(t, 0.0), 1.0);
-        const double y = __builtin_fma(t, steps, up), f = __builtin_fma(t, steps, up - y);
-        const unsigned n = (unsigned)__builtin_bit_cast(uint64_t, y);
-        double p = 3.3083026805413713e-09;
-        p = __builtin_fma(p, f, 3.665566060704036e-06);
-        p = __builtin_fma(p, f, 0.0027076061740622863);
-        p = __builtin_fma(p, f, 1.0);
+        const double at = NEAR ? __builtin_fma((double)x, c, shift) : __builtin_fma((double)x - top, c, (double)(kOctaves * kPowers));
+        unsigned n;
+        asm("v_cvt_u32_f64 %0, %1" : "=v"(n) : "v"(at));   // (what is out of range becomes the nearest, NaN 0: the language leaves both open)
+        const double f = __builtin_fmin(__builtin_fmax(__builtin_amdgcn_fract(at), 0.0), 1.0);   // (of -inf and NaN 0)
+        double p = 3.3127842005945513e-09;
+        p = __builtin_fma(p, f, 3.6655627958463705e-06);
+        p = __builtin_fma(p, f, 0.002707606174622391);
+        p = __builtin_fma(p, f, 0.9999999999999825);
         u32x2 power = powers[n & (kPowers - 1)];
         power[1] += n << 12;
         return __builtin_fma(p, __builtin_bit_cast(double, power), sum);
