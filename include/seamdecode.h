@@ -543,7 +543,8 @@ typedef struct {
  *   draw_logprobs   f32 [rows] or NULL: log(w / sum of the kept w), that of the draw
  *   workspace       >= sample_workspace_bytes(logits) bytes, contents ignored
  * -inf (and NaN) is never drawn.  +inf: the tokens that have it share all weight.  A row with no
- * logit above -inf gives token -1 and log probabilities of -inf.  vocab < 2^20 (SD_EUNSUPPORTED beyond).
+ * logit above -inf gives token -1 and log probabilities of -inf.  Where limits are given, logits further below the
+ * largest than fp32 reaches are not kept.  vocab < 2^20 (SD_EUNSUPPORTED beyond).
  */
 size_t sample_workspace_bytes(const sd_logits *shape);
 int sample_tokens(const sd_logits *shape, const void *logits, const float *temperature, const int32_t *top_k,
@@ -560,7 +561,8 @@ int sample_tokens(const sd_logits *shape, const void *logits, const float *tempe
  *
  *   targets       i32 [rows]; a row whose target is outside [0, vocab) is padding: its logits are not
  *                 read, its results are 0
- *   temperature   f32 [rows] or NULL: 1; 0, negative and NaN count as 1
+ *   temperature   f32 [rows] or NULL: 1; 0, negative and NaN count as 1, and positive ones are held to
+ *                 [2^-126, 2^125]; logits that are further apart than fp32 reaches count as infinitely far
  *   entropy       f32 [rows] or NULL
  *   stats         f32 [rows][2] or NULL: what the gradient needs
  *   workspace     >= token_logprobs_workspace_bytes(shape) bytes, contents ignored; the same for

@@ -121,17 +121,17 @@ SD_DEV float value_of(unsigned key)
 }
 
 struct RowLimits {
-    double c;
-    float temperature, top_p, min_p;
+    double temperature, c;
+    float top_p, min_p;
     int top_k;
     bool greedy, by_count, by_mass, by_least;
     SD_DEV RowLimits(const SampleArgs &a, int r)
     {
         temperature = a.temperature ? a.temperature[r] : 1.f;
-        greedy = !(temperature > 0.f);
-        if (greedy) temperature = 1.f;
-        temperature = min(temperature, 0x1p100f);   // no logits differ by so much, and those that are less apart weigh alike
-        c = kLog2e / (double)temperature;
+        greedy = !(temperature > 0.0);
+        if (greedy) temperature = 1.0;
+        temperature = __builtin_fmin(temperature, 0x1p200);   // (infinity: far above all differences, which 0 times -inf would not be)
+        c = kLog2e / temperature;
         top_k = a.top_k ? a.top_k[r] : 0;
         top_p = a.top_p ? a.top_p[r] : 1.f;
         min_p = a.min_p ? a.min_p[r] : 0.f;
@@ -246,7 +246,7 @@ SD_DEV void write_token(const SampleArgs &a, int64_t r, const Drawn &d, const Ro
     if (lane == 0) a.tokens[r] = d.token;
     float *to = lane == 0 ? a.logprobs : a.draw_logprobs;
     if (lane > 1 || !to) return;
-    const double z = d.x == t.top ? 0.0 : ((double)d.x - t.top) * (1.0 / (double)l.temperature);
+    const double z = d.x == t.top ? 0.0 : ((double)d.x - t.top) * (1.0 / l.temperature);
     to[r] = lane == 1 && l.greedy ? 0.f : (float)(z - log(lane == 0 ? t.sum : kept));
 }
 SD_DEV bool write_nothing(const SampleArgs &a, int64_t r, const RowTotal &t)
@@ -455,13 +455,13 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
     };
 
     // Bins of logits, from the largest down, 64 to the power of e; the last one's weights are 0.
-    float steps = min(64.f / l.temperature, 1e30f);
+    float steps = (float)__builtin_fmin(64.0 / l.temperature, 1e30);
     auto bin_of = [&](float x) { return (int)__builtin_fminf((top - x) * steps, (float)kFarBin); };
     int limit = kFarBin - 1;   // the last bin that may hold something that is kept
     auto bins_to = [](double weight) { return __builtin_fmin(-64.0 * log(weight), 1e6); };
     auto lower = [&](double least) { limit = min(limit, (int)(bins_to(least) * 1.00001) + 1); };   // nothing lighter than `least` is kept
     float sure = kInf;   // (top - x) up to which a logit is as heavy as min_p without doubt
-    if (l.by_least) sure = (float)(-log((double)l.min_p) * (double)l.temperature * 0.99999);
+    if (l.by_least) sure = (float)(-log((double)l.min_p) * l.temperature * 0.99999);
     if (l.by_least && !(l.by_count && l.by_mass)) lower((double)l.min_p);   // (top_p asks for a share of all that top_k leaves, light ones too)
     // All that are as light as this or lighter hold less than 1 - top_p: they come after.
     if (l.by_mass && !l.by_count) lower((1.0 - (double)l.top_p) * total.sum / (double)a.vocab);

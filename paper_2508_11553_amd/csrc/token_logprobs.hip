@@ -32,7 +32,7 @@ SD_DEV RowSums joined(RowSums a, RowSums b, float c)
 SD_DEV float log2_scale(const float *temperature, int64_t r)
 {
     const float t = temperature ? temperature[r] : 1.f;
-    return (float)(kLog2e / (t > 0.f ? __builtin_fmin(__builtin_fmax((double)t, 0x1p-126), 0x1p100) : 1.0));
+    return (float)(kLog2e / (t > 0.f ? __builtin_fmin(__builtin_fmax((double)t, 0x1p-126), 0x1p125) : 1.0));
 }
 
 SD_DEV void finish(const LogprobArgs &a, int64_t r, RowSums x, float c, float at_target)

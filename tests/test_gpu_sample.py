@@ -202,3 +202,32 @@ def test_outputs_that_are_not_asked_for(sd):
     tokens = torch.zeros(3, dtype=torch.int32, device="cuda")
     sd.sample_tokens(b.desc, b.flat, None, None, None, None, u, tokens, None, None, b.work, b.ws)
     assert np.array_equal(tokens.cpu().numpy(), b.draw(u.cpu().numpy())[0])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [300, 5000, 40001])
+def test_temperatures_and_logits_of_any_size(sd, kind, vocab):
+    """Temperatures at which all logits weigh alike though they differ, or only the largest weighs anything; logits so large that their neighbours are
+    whole temperatures away, or that differences pass the range of fp32; with every limit, few rows and many."""
+    rng = np.random.default_rng(vocab)
+    inf = np.inf
+    temperature = [inf, 1e30, 1e38, 1e-30, 1e-40, 1e-45, 1.0, 1e8, 1e9, 3e37, 1.0, 0.5]
+    rows = len(temperature)
+    x = rng.normal(0, 2, (rows, vocab))
+    x[6] *= 1e10
+    x[7] *= 1e10
+    x[8] = 1e10 + rng.integers(-3, 4, vocab) * 1e9
+    x[9] = rng.choice([-3e38, 3e38, 0.0, 1e38], vocab)
+    x[10] = 1e10 + rng.integers(0, 3, vocab)         # all equal once rounded
+    x[11] = -1e30
+    x[:, 5::11] = -inf
+    times = 1 if vocab > 10000 else 25
+    b = Batch(sd, np.tile(x, (times, 1)), kind)
+    for limits in (dict(), dict(top_k=7), dict(top_k=vocab // 2), dict(top_p=0.6), dict(top_p=0.999), dict(min_p=0.3), dict(top_k=vocab // 3, top_p=0.7, min_p=0.01)):
+        u = rng.random(rows * times).astype(np.float32)
+        got = b.draw(u, temperature=temperature * times, **{k: [v] * (rows * times) for k, v in limits.items()})
+        for r in range(rows * times if times == 1 else 3 * rows):
+            token, lp, dlp = plain.sample(b.x[r], np.float32(temperature[r % rows]), uniform=u[r], **{k: np.float32(v) if k != "top_k" else v for k, v in limits.items()})
+            assert got[0][r] == token, (r, limits, got[0][r], token)
+            for value, want in ((got[1][r], lp), (got[2][r], dlp)):
+                assert value == want or abs(value - want) <= 2.0 ** -24 * abs(want) + 1e-9, (r, limits, value, want)
