@@ -6,7 +6,7 @@
 // only what is left of them is written to it.
 //
 // Bound by latency: a small call is one workgroup's, which keeps all sums in LDS (64 sequences 6 us: counts, sums, pages, three trips to memory and five barriers); a
-// large one leaves them in the workspace for a second kernel (2048 sequences 5 us, then 8.5: counts -> sums into LDS -> search -> sequence -> page, each waits for
+// large one leaves them in the workspace for a second kernel (2048 sequences 5 us, then 6: counts -> sums into LDS -> search -> sequence -> page, each waits for
 // the one before; 200 sequences with 0.6 M rows 5 and 5.5).
 #include "logits.h"
 
@@ -165,6 +165,22 @@ SD_DEV int last_not_above(const T *s_from, const T *from, int stride, int n, T x
     return lo;
 }
 
+// Every `stride`-th of n entries into LDS, four loads of a thread on their way together.
+template <typename T>
+SD_DEV void hold(T *s_from, const T *from, int stride, int n)
+{
+    constexpr int kAtOnce = 4;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kAtOnce * 256) {
+        T x[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) x[j] = from[min(i0 + j * 256 + (int)threadIdx.x, n - 1) * stride];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (i0 + j * 256 + (int)threadIdx.x < n) s_from[i0 + j * 256 + threadIdx.x] = x[j];
+    }
+}
+
 // The i-th page of the list, where it came back: of sequence b, of length L.
 SD_DEV int returned_page(const PlanArgs &a, int b, int L, int64_t nth) { return a.block_table[(int64_t)b * a.max_blocks + own_from(a, b, L) + nth]; }
 
@@ -250,7 +266,7 @@ __global__ __launch_bounds__(256) void plan_fill_kernel(PlanArgs a)
         const int rows = a.row_start[a.B];
         const int64_t row0 = (int64_t)blockIdx.x * 1024, t = row0 + kPer * tid;
         if (row0 < rows) {
-            for (int i = tid; i < sample; i += 256) s_from[i] = a.row_start[i * stride];
+            hold(s_from, a.row_start, stride, sample);
             __syncthreads();
         }
         if (t >= a.max_rows) return;
@@ -279,25 +295,20 @@ __global__ __launch_bounds__(256) void plan_fill_kernel(PlanArgs a)
     const int64_t items = pages + max(left - held, (int64_t)0);
     const int64_t at = (int64_t)(blockIdx.x - row_blocks) * 256, step = (int64_t)(gridDim.x - row_blocks) * 256;
     if (at >= items) return;
-    for (int i = tid; i < sample; i += 256) s_from[i] = a.page_from[i * stride];
-    if (back > 0)
-        for (int i = tid; i < sample; i += 256) s_back[i] = a.back_from[i * stride];
+    hold(s_from, a.page_from, stride, sample);
+    if (back > 0) hold(s_back, a.back_from, stride, sample);
     __syncthreads();
     for (int64_t i = at + tid; i < items; i += step) {
         const int64_t place = i < pages ? available - 1 - i : held + i - pages;   // in the list
-        int page;
-        if (place < held) {
-            page = a.free_pages[place];
-        } else {
-            const int b = last_not_above<int64_t>(s_back, a.back_from, stride, a.B, place - held);
-            page = returned_page(a, b, a.starts[b], place - held - a.back_from[b]);
-        }
-        if (i < pages) {
-            const int b = last_not_above<int>(s_from, a.page_from, stride, a.B, (int)i);
-            a.block_table[(int64_t)b * a.max_blocks + pages_of(a.starts[b]) + (i - a.page_from[b])] = page;
-        } else {
-            a.free_pages[place] = page;
-        }
+        const bool taken = i < pages, listed = place < held;
+        // (both searches before the loads that they lead to)
+        const int to = taken ? last_not_above<int>(s_from, a.page_from, stride, a.B, (int)i) : 0;
+        const int from = listed ? 0 : last_not_above<int64_t>(s_back, a.back_from, stride, a.B, place - held);
+        const int start = a.starts[to], first = a.page_from[to], length = a.starts[from];
+        const int64_t returned = a.back_from[from];
+        const int page = listed ? a.free_pages[place] : returned_page(a, from, length, place - held - returned);
+        if (taken) a.block_table[(int64_t)to * a.max_blocks + pages_of(start) + (i - first)] = page;
+        else a.free_pages[place] = page;
     }
 }
 
