@@ -231,3 +231,28 @@ def test_temperatures_and_logits_of_any_size(sd, kind, vocab):
             assert got[0][r] == token, (r, limits, got[0][r], token)
             for value, want in ((got[1][r], lp), (got[2][r], dlp)):
                 assert value == want or abs(value - want) <= 2.0 ** -24 * abs(want) + 1e-9, (r, limits, value, want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(3, 2 ** 20 - 1), (2, 524289), (300, 270001)])
+def test_the_largest_vocabularies(sd, kind, rows, vocab):
+    """More lanes' maxima than the threads hold at once, more stretches than a wave has lanes; peaked rows and nearly even ones."""
+    import torch
+    rng = np.random.default_rng(rows)
+    some = sorted({0, 1, rows - 1})
+    x = np.zeros((rows, vocab), np.float32)
+    for r in some:
+        x[r] = rng.normal(0, 0.5 if r else 2, vocab)
+    x[0, rng.integers(0, vocab, 30)] = 12 + rng.normal(0, 1, 30)
+    x[0, vocab - 1] = 14.0
+    b = Batch(sd, x, kind)
+    for limits in (dict(), dict(top_k=40, top_p=0.9), dict(top_p=0.95), dict(top_k=vocab // 2), dict(min_p=0.2)):
+        u = rng.random(rows).astype(np.float32)
+        got = b.draw(u, **{k: [v] * rows for k, v in limits.items()})
+        for r in some:
+            token, lp, dlp = plain.sample(b.x[r], uniform=u[r], **{k: np.float32(v) if k != "top_k" else v for k, v in limits.items()})
+            assert got[0][r] == token, (r, limits, got[0][r], token)
+            for value, want in ((got[1][r], lp), (got[2][r], dlp)):
+                assert abs(value - want) <= 2.0 ** -24 * abs(want) + 1e-9, (r, limits, value, want)
+    del b
+    torch.cuda.empty_cache()
