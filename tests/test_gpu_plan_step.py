@@ -191,3 +191,39 @@ def test_counts_out_of_range(sd):
     p.d["block_table"][0, :3] = torch.tensor([-7, 2 ** 31 - 1, 1000], dtype=torch.int32, device="cuda")
     p.table[0][:3] = [-7, 2 ** 31 - 1, 1000]
     p.step([-1, 17], max_rows=17)
+
+
+def test_places_of_a_quantised_cache(sd):
+    """The plan's starts and row_start as kv_append_fp8 takes them, its slots as kv_append does: what every sequence then holds is what it holds on pages chosen by hand."""
+    import torch
+    B, heads, d, blocks, pages = 6, 2, 64, 9, 60
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    dev = lambda a: torch.tensor(np.asarray(a, np.int32), device="cuda")  # noqa: E731
+    shapes = [sd.Shape(batch=B, num_q_heads=heads, num_kv_heads=heads, head_dim=d, page_size=16, num_pages=pages, max_blocks_per_seq=blocks, kv_dtype=kind, max_context_len=16 * blocks,
+                       chunk_tokens=0) for kind in (sd.SD_FP8_E4M3, sd.SD_BF16)]
+    own, hand = i32(B, blocks), torch.arange(B * blocks, dtype=torch.int32, device="cuda").view(B, blocks)
+    pools = [[torch.zeros((pages, heads, 16, d), dtype=t, device="cuda") for t in (torch.uint8, torch.uint8, torch.int16, torch.int16)] +
+             [torch.zeros((pages, heads), device="cuda") for _ in range(2)] for _ in range(2)]
+    lens, free_pages, free, work = i32(B), torch.randperm(pages, generator=gen, device="cuda").int(), dev([pages]), torch.empty(4096, dtype=torch.uint8, device="cuda")
+    granted, row_start, starts, every = i32(B), i32(B + 1), i32(B), dev(range(B))
+    held = [0] * B
+    for new in ([40, 3, 16, 0, 100, 1], [1, 17, -1, 5, 1, 1], [7, 1, 33, 1, -1, 15], [1, 1, 1, 1, 20, 1]):
+        rows = sum(n for n in new if n > 0)
+        seq, slots = i32(rows), i32(rows)
+        sd.kv_plan_step(shapes[0], dev(new), None, lens, lens, None, None, free_pages, free, free, own, rows, granted, row_start, starts, seq, slots, None, work, 4096)
+        k, v = (torch.randn((rows, heads, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+        host = dict(seq=[b for b, n in enumerate(new) for _ in range(max(n, 0))], slots=[held[b] + i for b, n in enumerate(new) for i in range(max(n, 0))],
+                    start=list(held), row0=[sum(max(n, 0) for n in new[:b]) for b in range(B + 1)])
+        for (kq, vq, kb, vb, ks, vs), table, places in ((pools[0], own, (seq, slots, starts, row_start)), (pools[1], hand, [dev(host[n]) for n in ("seq", "slots", "start", "row0")])):
+            sd.kv_append_fp8(shapes[0], k, v, every, places[2], places[3], B, max(new), kq, vq, ks, vs, table)
+            sd.kv_append(shapes[1], k, v, places[0], places[1], rows, kb, vb, table)
+        held = [0 if n < 0 else h + n for h, n in zip(held, new)]
+        assert lens.tolist() == held
+        for b, n in enumerate(held):
+            used = (n + 15) // 16
+            for i, (x, y) in enumerate(zip(*pools)):
+                x, y = x[own[b, :used].long()], y[hand[b, :used].long()]
+                if x.dim() == 4:
+                    x, y = (z.transpose(1, 2).reshape(-1, heads, d)[:n] for z in (x, y))
+                assert torch.equal(x, y), (new, b, i)
