@@ -543,8 +543,7 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
         __syncthreads();
     }
     int listed = s_n[1];
-    const bool complete = found_groups <= kGroups && listed <= kList;   // the list holds all down to the limit
-    bool from_list = complete;
+    bool complete = found_groups <= kGroups && listed <= kList;   // the list holds all down to the limit
 
     // Rows that are gone over: a wave a part of the row, the next kBatch of its vectors on their way.  A stretch may lie in two waves' parts.
     auto each_vector = [&](auto &&use, auto &&ends) {   // use(vector, index of its first logit)
@@ -593,6 +592,7 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
     bool summed = false;    // s_stretch holds the weights of what lies in bins before `split`, the list all the others that may be kept
     int split = 0;
     uint64_t base = 0;      // the weight of what lies before `split`, light or not
+    int ahead = 0;          // how many lie before it, where only those are counted
     auto stays = [&](float x, int i) {
         const int bin = bin_of(x);
         return (bin < split || (bin <= limit && kept(key_of<F32>(x), i))) && heavy(x);
@@ -679,6 +679,45 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
         return aim > base ? aim - base : 1;
     };
 
+    if ((complete || summed) && listed > kRanked && (l.by_count || l.by_mass)) {
+        // Fewer: what lies past the bin in which the count, or the share, ends leaves the list; and where that is not enough what lies before it too, as it stays.
+        clear_bins();
+        for (int i = tid; i < listed; i += kChooseThreads) {
+            const float x = value_of<F32>((unsigned)(s_list[i] >> 32));
+            if (bin_of(x) <= limit) add_to_bin(bin_of(x), l.by_count ? 1 : weigh.whole(x));
+        }
+        const Found f = find(l.by_count ? (uint64_t)l.top_k : mass_aim());
+        if (f.some) {
+            limit = f.bin;
+            for (int round = 0; round < 2; ++round) {
+                const int from = round ? limit : 0;
+                if (listed <= kRanked || (round && (limit == 0 || (l.by_count && l.by_mass)))) break;   // (a share of what the count leaves is not known yet)
+                uint64_t mine[kList / kChooseThreads];
+#pragma unroll
+                for (int j = 0; j < kList / kChooseThreads; ++j) mine[j] = tid + j * kChooseThreads < listed ? s_list[tid + j * kChooseThreads] : 0;
+                if (tid == 0) s_n[1] = 0;
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < kList / kChooseThreads; ++j) {
+                    const float x = value_of<F32>((unsigned)(mine[j] >> 32));
+                    const int bin = bin_of(x);
+                    if (tid + j * kChooseThreads >= listed || bin > limit) continue;
+                    if (bin >= from) s_list[atomicAdd(&s_n[1], 1)] = mine[j];
+                    else if (heavy(x)) atomicAdd(reinterpret_cast<ull *>(&s_stretch[(int)~(unsigned)mine[j] / kStretch]), (ull)weigh.whole(x));
+                }
+                __syncthreads();
+                listed = s_n[1];
+                if (round) {
+                    complete = false;
+                    summed = true;
+                    split = from;
+                    if (l.by_count) ahead = (int)f.before;
+                    else base += f.before;
+                }
+                __syncthreads();
+            }
+        }
+    }
     if ((complete || summed) && listed <= kRanked && (l.by_count || l.by_mass)) {
         // Few: each one's rank is counted, the threads of a candidate sharing the others.
         const int width = listed <= 64 ? 64 : listed <= 128 ? 128 : 256, shares = kChooseThreads / width;
@@ -696,7 +735,7 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
         __syncthreads();
         // by every wave alike
         uint64_t x[4], sum = 0;
-        const int most = l.by_count ? min(l.top_k, listed) : listed;
+        const int most = l.by_count ? min(l.top_k - ahead, listed) : listed;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum += x[e] = 4 * lane + e < most ? s_bins[4 * lane + e] : 0;
         const uint64_t ends = wave_scan64(sum);
@@ -745,6 +784,7 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
         }
     } else if (l.by_count || l.by_mass) {
         // By histograms, of the list or of the row.
+        bool from_list;
         auto each = [&](auto &&use) {
             if (from_list) {
                 for (int i = tid; i < listed; i += kChooseThreads) {
@@ -764,7 +804,7 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
                 const int bin = bin_of(x);
                 if (bin <= limit && kept(key, i)) add_to_bin(bin, mass ? weigh.whole(x) : 1);
             });
-            uint64_t aim = (uint64_t)l.top_k;
+            uint64_t aim = (uint64_t)(l.top_k - ahead);
             if (mass) {
                 aim = mass_aim();
                 if (l.by_count) {   // of what the count left

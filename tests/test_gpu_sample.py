@@ -256,3 +256,21 @@ def test_the_largest_vocabularies(sd, kind, rows, vocab):
                 assert abs(value - want) <= 2.0 ** -24 * abs(want) + 1e-9, (r, limits, value, want)
     del b
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [257, 300, 700, 2047, 2048, 2049, 3100])
+@pytest.mark.parametrize("step", [0, 0.25, 0.002])
+def test_hundreds_are_kept(sd, kind, vocab, step):
+    """Candidates by the hundred: a limit ends within a bin of nearly equal ones, among equal ones (logits in steps), or past all of them; each limit alone and with others."""
+    rng = np.random.default_rng(vocab)
+    rows = 7
+    x = rng.normal(0, 0.6, (rows, vocab))
+    if step:
+        x = np.round(x / step) * step
+    b = Batch(sd, x, kind)
+    k = [256, 257, 300, min(500, vocab), vocab // 2 + 1, vocab - 1, 2]
+    p = [0.5, 0.9, 0.99, 0.999, 0.3, 0.7, 0.97]
+    m = [0.05, 0.1, 0.2, 0.01, 0.3, 0.02, 0.15]
+    for use in (dict(top_k=k), dict(top_p=p), dict(top_k=k, top_p=p), dict(top_k=k, min_p=m), dict(top_p=p, min_p=m), dict(top_k=k, top_p=p, min_p=m), dict(min_p=m)):
+        check(b, rng.random(rows).astype(np.float32), temperature=rng.uniform(0.4, 1.3, rows), **use)
