@@ -222,16 +222,19 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(PlanArgs a)
         const int b = last_not_above<int>(s_page, nullptr, 1, a.B, i);
         a.block_table[(int64_t)b * a.max_blocks + pages_of(s_start[b]) + (i - s_page[b])] = page_at(available - 1 - i);
     }
-    const int64_t left = min(available - pages, (int64_t)a.num_pages);
+    const int64_t left = min(available - pages, (int64_t)a.num_pages) - held;   // of the pages that came back
     constexpr int kAtOnce = 4;
-    for (int64_t i0 = held + tid; i0 < left; i0 += kAtOnce * THREADS) {
-        int page[kAtOnce];
+    for (int64_t i0 = kAtOnce * tid; i0 < left; i0 += kAtOnce * THREADS) {   // (mostly of one sequence: found once)
+        int b = last_not_above<int64_t>(s_back, nullptr, 1, a.B, i0), page[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (i0 + j >= left) break;
+            while (b + 1 < a.B && s_back[b + 1] <= i0 + j) ++b;
+            page[j] = returned_page(a, b, s_start[b], i0 + j - s_back[b]);
+        }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
-            if (i0 + j * THREADS < left) page[j] = page_at(i0 + j * THREADS);
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j)
-            if (i0 + j * THREADS < left) a.free_pages[i0 + j * THREADS] = page[j];
+            if (i0 + j < left) a.free_pages[held + i0 + j] = page[j];
     }
 }
 
@@ -314,7 +317,10 @@ __global__ __launch_bounds__(256) void plan_fill_kernel(PlanArgs a)
 
 hipError_t launch_plan(const PlanArgs &a, hipStream_t stream)
 {
-    if (a.B <= 256 * kPer && a.max_rows <= 1024) {
+    // One workgroup is sooner while few pages come back, two kernels take the same whatever comes back.  us, one : two: 64 sequences 6.4 : 9.2, 3 of them finished with 900
+    // pages 10.2 : 9.8, 6 with 7 k pages 22.6 : 9.9; 512 7.2 : 9.6; 1000 9.0 : 10.4, 100 of them finished with 6.5 k pages 35 : 10.5, 300 with 95 k 173 : 10.6.  In a rollout as
+    // many pages come back as are taken, one in 16 tokens, though some steps see many: few sequences, one workgroup.
+    if (a.B <= 256 && a.max_rows <= 1024) {
         hipLaunchKernelGGL((plan_kernel<256>), dim3(1), dim3(256), 0, stream, a);
     } else {
         if (a.B <= 256 * kPer) hipLaunchKernelGGL(plan_sums_kernel<256>, dim3(1), dim3(256), 0, stream, a);
