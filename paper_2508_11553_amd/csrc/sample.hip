@@ -633,8 +633,9 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
         double sum = kNone;
         uint64_t all = 0;
         const float upper = (float)split, lower_end = (float)(limit + 1);
-        auto sum_up = [&](auto quick) {
-            constexpr bool kQuick = decltype(quick)::value;
+        // (added as `whole` rounds them: the walk to the token has to come to the same sum)
+        auto sum_up = [&](auto quick, auto near) {
+            constexpr bool kQuick = decltype(quick)::value, kNear = decltype(near)::value;
             each_vector([&](u32x4 w, int first) {
                 float x[Row::kEach];
                 bool other = false;   // something is left over, or may be light
@@ -657,7 +658,7 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < Row::kEach; ++e) sum = weigh.template add<kQuick>(sum, x[e]);
+                for (int e = 0; e < Row::kEach; ++e) sum = weigh.template add<kNear>(sum, x[e]);
             }, [&](int s) {
                 const uint64_t whole = wave_scan64(__builtin_bit_cast(uint64_t, sum) - kNoneBits);
                 if (lane == 63) atomicAdd(reinterpret_cast<ull *>(&s_stretch[s]), (ull)whole);
@@ -665,8 +666,9 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
                 sum = kNone;
             });
         };
-        if (weigh.near && !lone.on && !l.by_least) sum_up(std::true_type());
-        else sum_up(std::false_type());
+        if (!weigh.near) sum_up(std::false_type(), std::false_type());
+        else if (lone.on || l.by_least) sum_up(std::false_type(), std::true_type());
+        else sum_up(std::true_type(), std::true_type());
         all = wave_scan64(all);
         if (lane == 63) atomicAdd(reinterpret_cast<ull *>(&s_base), (ull)all);
         __syncthreads();
