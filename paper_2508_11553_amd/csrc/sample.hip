@@ -603,13 +603,14 @@ __global__ __launch_bounds__(THREADS) void sample_choose_kernel(SampleArgs a)
         // The bin in which the share ends, from weights in 32 bits: whole ones of 2^-31 of the row's, each off by less than one and 2^-16 of itself.
         steps *= (float)(kBins - 2) / (float)(limit + 1);
         limit = kBins - 2;
-        const float to_exponent = (float)-l.c, whole = (float)(31.0 - log2(total.sum));
+        // (exponents from bins: log2(e) / temperature may pass the range of fp32, bins to octaves does not; no steps: all weigh alike)
+        const float to_exponent = steps > 0.f ? (float)(-l.c / (double)steps) : 0.f, whole = (float)(31.0 - log2(total.sum));
         unsigned *bins = reinterpret_cast<unsigned *>(s_bins);
         clear_bins();
         const float past = (float)(limit + 1);
         auto add_up = [&](float x, int) {
             const float d = top - x, bin = d * steps;
-            const unsigned w = (unsigned)__builtin_amdgcn_exp2f(__builtin_fmaf(d, to_exponent, whole));
+            const unsigned w = (unsigned)__builtin_amdgcn_exp2f(__builtin_fmaf(bin, to_exponent, whole));
             if (bin < past) atomicAdd(&bins[2 * (int)bin + lane % 2], w);   // (two of each bin: logits crowd)
         };
         if (lone.on) each_logit(add_up, [](int) {});
