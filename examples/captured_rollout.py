@@ -20,13 +20,26 @@ import paper_2508_11553_amd as sd  # noqa: E402
 from bounded_rollout import PAGE, Layer, NormRope  # noqa: E402
 
 
+def side_by_side(x):
+    """x as the calls take it: without gaps, from 16 bytes on."""
+    return x if x is None or (x.is_contiguous() and x.data_ptr() % 16 == 0) else x.clone(memory_format=torch.contiguous_format)
+
+
 class TokenLogprobs(torch.autograd.Function):
     """Log probabilities of `targets` [T] (< 0: padding) under the rows of `logits` [T][vocab], and the rows' entropies."""
 
     @staticmethod
     def forward(ctx, logits, targets, temperature):
+        if logits.dtype not in (torch.bfloat16, torch.float32) or targets.dtype != torch.int32 or (temperature is not None and temperature.dtype != torch.float32):
+            raise TypeError("logits are bf16 or fp32, targets int32, temperatures fp32")
+        if logits.dim() != 2 or logits.shape[1] == 0 or targets.shape != logits.shape[:1] or (temperature is not None and temperature.shape != targets.shape):
+            raise ValueError("logits are [T][vocab], targets and temperatures [T]")
         rows, vocab = logits.shape
-        desc = sd.Logits(rows=rows, vocab=vocab, dtype=sd.SD_BF16 if logits.dtype == torch.bfloat16 else sd.SD_F32, stride=logits.stride(0))
+        # (the calls take rows of logits that lie apart, but no other gaps)
+        taken = logits.stride(1) == 1 and logits.stride(0) >= vocab and logits.data_ptr() % 16 == 0
+        logits = logits if taken else logits.clone(memory_format=torch.contiguous_format)
+        targets, temperature = side_by_side(targets), side_by_side(temperature)
+        desc = sd.Logits(rows=rows, vocab=vocab, dtype=sd.SD_BF16 if logits.dtype == torch.bfloat16 else sd.SD_F32, stride=logits.stride(0) if taken else 0)
         logprobs, entropy = (torch.empty(rows, device=logits.device) for _ in range(2))
         stats = torch.empty((rows, 2), device=logits.device)
         ws = sd.token_logprobs_workspace_bytes(desc)
@@ -39,7 +52,7 @@ class TokenLogprobs(torch.autograd.Function):
     def backward(ctx, d_logprobs, d_entropy):
         logits, targets, temperature, stats, entropy = ctx.saved_tensors
         d_logits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=logits.device)
-        sd.token_logprobs_backward(ctx.desc, logits, targets, temperature, stats, entropy, d_logprobs.contiguous(), d_entropy.contiguous(), d_logits)
+        sd.token_logprobs_backward(ctx.desc, logits, targets, temperature, stats, entropy, side_by_side(d_logprobs), side_by_side(d_entropy), d_logits)
         return d_logits, None, None
 
 
