@@ -138,9 +138,8 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a
     const LogitRow<F32> out(a.d_logits, r, a.stride, a.vocab);
     const float c = log2_scale(a.temperature, r), inverse = c * (float)kLn2;
     const float m = a.stats[2 * (int64_t)r], log2_sum = a.stats[2 * (int64_t)r + 1];
-    const float g = padding ? 0.f : a.d_logprobs[r] * inverse, h = padding || !a.d_entropy ? 0.f : a.d_entropy[r] * inverse;
-    const float of_h = a.d_entropy && !padding ? a.entropy[r] : 0.f;
-    const float base = g + h * of_h, slope = h * (float)kLn2, at_target = log2_sum == __builtin_inff() ? 0.f : g;
+    const float g = padding ? 0.f : a.d_logprobs[r], h = padding || !a.d_entropy ? 0.f : a.d_entropy[r];
+    const float entropy = a.d_entropy && !padding ? a.entropy[r] : 0.f, at_target = log2_sum == __builtin_inff() ? 0.f : g;
     const int v0 = (int)part * kGradVectors * 256 + (int)threadIdx.x;
     u32x4 w[kGradVectors];
     if (!padding) {
@@ -156,7 +155,9 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a
 #pragma unroll
         for (int e = 0; e < Row::kEach; ++e) {
             const float z = max_of((Row::value(w[j], e) - m) * c - log2_sum, kFar), q = __builtin_amdgcn_exp2f(z);   // log2 p, p
-            y[e] = padding ? 0.f : -q * (base + slope * z) + (v * Row::kEach + e == target ? at_target : 0.f);
+            // (p goes into each product first: what has no weight stays 0 whatever g, h and 1 / temperature come to; a p below 2^-126 has none)
+            const float share = __builtin_fmaf(h, q * __builtin_fmaf(z, (float)kLn2, entropy), q * g);
+            y[e] = padding ? 0.f : ((v * Row::kEach + e == target ? at_target : 0.f) - share) * inverse;
         }
         u32x4 to;
 #pragma unroll
