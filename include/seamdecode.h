@@ -539,7 +539,9 @@ typedef struct {
  *   uniform         f32 [rows], in [0, 1); below (or NaN) counts as 0, from 1 on as just below 1
  *   tokens          i32 [rows], written
  *   logprobs        f32 [rows] or NULL: log(w / sum of all w), the token's log probability at the
- *                   row's temperature; what token_logprobs gives for it
+ *                   row's temperature; what token_logprobs gives for it, but for rows with NaN or +inf (NaN
+ *                   there), temperatures outside [2^-126, 2^125] (held to that there, taken as they are here)
+ *                   and logits that are further apart than fp32 reaches (infinitely far there)
  *   draw_logprobs   f32 [rows] or NULL: log(w / sum of the kept w), that of the draw
  *   workspace       >= sample_workspace_bytes(logits) bytes, contents ignored
  * -inf (and NaN) is never drawn.  +inf: the tokens that have it share all weight.  A row with no
