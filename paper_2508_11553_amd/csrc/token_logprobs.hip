@@ -156,8 +156,8 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a
         for (int e = 0; e < Row::kEach; ++e) {
             const float z = max_of((Row::value(w[j], e) - m) * c - log2_sum, kFar), q = __builtin_amdgcn_exp2f(z);   // log2 p, p
             // (p goes into each product first: what has no weight stays 0 whatever g, h and 1 / temperature come to; a p below 2^-126 has none)
-            const float share = __builtin_fmaf(h, q * __builtin_fmaf(z, (float)kLn2, entropy), q * g);
-            y[e] = padding ? 0.f : ((v * Row::kEach + e == target ? at_target : 0.f) - share) * inverse;
+            const float of_target = v * Row::kEach + e == target ? at_target : 0.f, of_g = __builtin_fmaf(-q, g, of_target);
+            y[e] = padding ? 0.f : __builtin_fmaf(-h, q * __builtin_fmaf(z, (float)kLn2, entropy), of_g) * inverse;
         }
         u32x4 to;
 #pragma unroll
