@@ -605,6 +605,10 @@ int token_logprobs_backward(const sd_logits *shape, const void *logits, const in
  * Pages that come back are free for this call's other sequences.  Sequences are served in the batch's order: with all that was asked
  * for up to and including b summed up, b gets its slots if the free pages suffice (or it needs
  * none) and its rows fit max_rows; else, and where L + n exceeds max_context_len, it waits.
+ * What waits for pages or rows counts all the same: a request that the free pages or max_rows cannot serve holds
+ * back every later sequence that wants a page (or, past max_rows, anything), in every call that repeats it.  A caller asks
+ * for no more than can be served, in pieces if need be, or puts first what is not to wait.  (L + n beyond
+ * max_context_len is not counted.)
  *
  *   new_tokens          i32 [batch]
  *   shared_len          i32 [batch] or NULL: zeros

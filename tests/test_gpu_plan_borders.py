@@ -56,3 +56,18 @@ def test_more_pages_are_taken_than_threads(sd, spare):  # noqa: F811
     p = Plan(sd, lens, 350, spare, 9)
     p.step(new, max_rows=1024)
     pages_once(p)
+
+
+@pytest.mark.parametrize("others", [9, 300])
+def test_what_waits_holds_back_what_follows(sd, others):  # noqa: F811
+    """The first asks for more pages than there are: in every call those behind it that need a page wait, those that need none go on.  In pieces all are served; a length
+    that no sequence may have is not counted."""
+    lens = [0] + [16 if i % 10 == 0 else 17 + i % 10 for i in range(others)]
+    ones = [1] * others
+    p = Plan(sd, lens, 100, 80, 4)
+    assert p.step([1601] + ones, max_rows=4000)["granted"] == [0] + ones
+    p = Plan(sd, lens, 100, 80, 4)
+    for _ in range(2):
+        goes = [int(n % 16 != 0) for n in p.lens[1:]]
+        assert p.step([1584] + ones, max_rows=4000)["granted"] == [0] + goes and 0 in goes
+    assert p.step([80] + ones, max_rows=4000)["granted"] == [80] + ones
