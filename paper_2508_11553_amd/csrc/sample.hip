@@ -26,6 +26,9 @@
 
 #include <type_traits>
 
+// Products are fused where the code says so and nowhere else: what one kernel sums another one walks, and both have to round alike.
+#pragma clang fp contract(off)
+
 namespace sd {
 
 namespace {
@@ -77,7 +80,7 @@ struct Weigher {
     const u32x2 *powers;
     bool near;
     SD_DEV Weigher(float top_, double c_, const u32x2 *powers_)
-        : top(top_), c(c_ * kPowers), shift(kOctaves * kPowers - top * c), powers(powers_), near(__builtin_fabs(top * c) < 65536.0)
+        : top(top_), c(c_ * kPowers), shift(__builtin_fma(-top, c, (double)(kOctaves * kPowers))), powers(powers_), near(__builtin_fabs(top * c) < 65536.0)
     {
     }
     SD_DEV double weight(float x) const { return exp2_of(((double)x - top) * (c * (1.0 / kPowers))); }   // (of the largest exactly 1)

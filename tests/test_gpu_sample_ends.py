@@ -30,3 +30,24 @@ def test_a_uniform_number_of_one_takes_the_last_kept_token(sd, kind, rows, vocab
         part = Batch(sd, x[some], kind)
         same = check(part, u[some], temperature=[t] * len(u[some]), top_p=p[some], min_p=None if min_p is None else min_p[some])
         assert all(np.array_equal(y[some], z) for y, z in zip(got, same))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [70, 2048, 6001])
+def test_a_uniform_number_of_one_without_limits_takes_the_last_token(sd, kind, vocab):  # noqa: F811
+    """Thousands of rows whose every token has weight: the kernel that sums a stretch and those that walk it come to the same sum, whatever limits are given that
+    do not limit, for few rows and for many."""
+    rng = np.random.default_rng(vocab)
+    rows = 20000 if vocab < 5000 else 6000
+    x = (rng.normal(0, 1, (rows, vocab)) + rng.normal(0, 10, (rows, 1))).astype(np.float32)
+    t = rng.uniform(0.5, 1.5, rows)
+    u = np.ones(rows, np.float32)
+    b = Batch(sd, x, kind)
+    want = b.draw(u, temperature=t)
+    assert (want[0] == vocab - 1).all(), np.flatnonzero(want[0] != vocab - 1)[:5]
+    many = b.draw(u, temperature=t, top_p=np.ones(rows))
+    assert all(np.array_equal(y, z) for y, z in zip(many, want))
+    for first in range(0, rows, rows // 8):
+        at = slice(first, first + 256)
+        few = Batch(sd, x[at], kind).draw(u[at], temperature=t[at], top_p=np.ones(256))
+        assert all(np.array_equal(y, z[at]) for y, z in zip(few, want))
