@@ -569,7 +569,8 @@ int sample_tokens(const sd_logits *shape, const void *logits, const float *tempe
  *   stats         f32 [rows][2] or NULL: what the gradient needs
  *   workspace     >= token_logprobs_workspace_bytes(shape) bytes, contents ignored; the same for
  *                 every shape
- * A target of -inf has the log probability -inf; a row of nothing else -inf and the entropy 0; NaN or +inf in a row
+ * A target of -inf has the log probability -inf (one masked by the type's lowest number a finite one, where fp32
+ * holds it); a row of nothing else -inf and the entropy 0; NaN or +inf in a row
  * makes its results NaN.  vocab < 2^30 (SD_EUNSUPPORTED beyond).
  */
 size_t token_logprobs_workspace_bytes(const sd_logits *shape);

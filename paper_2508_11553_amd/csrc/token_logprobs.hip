@@ -28,19 +28,20 @@ SD_DEV RowSums joined(RowSums a, RowSums b, float c)
     const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
     return RowSums{m, a.s * ea + b.s * eb, (a.t + a.s * da) * ea + (b.t + b.s * db) * eb};
 }
-// log2(e) / temperature; finite and not 0, so that it times a difference of 0 is 0 and times one of -inf is -inf.
-SD_DEV float log2_scale(const float *temperature, int64_t r)
+// log2(e) / temperature; in fp32 finite and not 0, so that it times a difference of 0 is 0 and times one of -inf is -inf.
+SD_DEV double log2_scale(const float *temperature, int64_t r)
 {
     const float t = temperature ? temperature[r] : 1.f;
-    return (float)(kLog2e / (t > 0.f ? __builtin_fmin(__builtin_fmax((double)t, 0x1p-126), 0x1p125) : 1.0));
+    return kLog2e / (t > 0.f ? __builtin_fmin(__builtin_fmax((double)t, 0x1p-126), 0x1p125) : 1.0);
 }
 
-SD_DEV void finish(const LogprobArgs &a, int64_t r, RowSums x, float c, float at_target)
+SD_DEV void finish(const LogprobArgs &a, int64_t r, RowSums x, double c, float at_target)
 {
     const float log2_sum = x.s > 0.f || x.s != x.s ? (float)log2((double)x.s) : -__builtin_inff();
     const bool nothing = log2_sum == -__builtin_inff();   // every logit is -inf
-    const float z = (at_target - x.m) * c;
-    a.logprobs[r] = nothing ? log2_sum : (float)(((double)z - log2_sum) * kLn2);
+    // (in 64 bits: of a target masked by the type's lowest number 2-based logarithms pass the range of fp32, the result does not)
+    const double z = ((double)at_target - x.m) * c;
+    a.logprobs[r] = nothing ? log2_sum : (float)((z - log2_sum) * kLn2);
     if (a.entropy) a.entropy[r] = nothing ? 0.f : (float)((log2_sum - (double)x.t / x.s) * kLn2);
     // What the gradient needs: the largest logit and log2 of the sum; of a row with nothing a sum past all, which leaves no weight.
     if (a.stats) a.stats[2 * r] = nothing ? 0.f : x.m, a.stats[2 * r + 1] = nothing ? __builtin_inff() : log2_sum;
@@ -73,7 +74,8 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a)
         return;
     }
     const Row row(a.logits, r, a.stride, a.vocab);
-    const float c = log2_scale(a.temperature, r), at_target = row.at(target);
+    const double to_log2 = log2_scale(a.temperature, r);
+    const float c = (float)to_log2, at_target = row.at(target);
     const int per_part = (row.vectors + a.slices - 1) / a.slices;
     const int end = min(row.vectors, (int)(part + 1) * per_part);
     RowSums x{kLowest, 0.f, 0.f};
@@ -106,7 +108,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobArgs a)
     if (wave != 0) return;
     x = join_lanes<kWaves>(lane < kWaves ? s_wave[lane] : RowSums{kLowest, 0.f, 0.f}, c);
     if (lane != 0) return;
-    if (a.slices == 1) finish(a, r, x, c, at_target);
+    if (a.slices == 1) finish(a, r, x, to_log2, at_target);
     else a.parts[3 * (int64_t)blockIdx.x] = x.m, a.parts[3 * (int64_t)blockIdx.x + 1] = x.s, a.parts[3 * (int64_t)blockIdx.x + 2] = x.t;
 }
 
@@ -117,14 +119,15 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a)
     const int64_t r = blockIdx.x;
     const int target = a.targets[r];
     if ((unsigned)target >= (unsigned)a.vocab) return;
-    const float c = log2_scale(a.temperature, r), at_target = LogitRow<F32>(a.logits, r, a.stride, a.vocab).at(target);
+    const double to_log2 = log2_scale(a.temperature, r);
+    const float c = (float)to_log2, at_target = LogitRow<F32>(a.logits, r, a.stride, a.vocab).at(target);
     RowSums x{kLowest, 0.f, 0.f};
     for (int i = threadIdx.x; i < a.slices; i += 64) {
         const float *p = a.parts + 3 * (r * a.slices + i);
         x = joined(x, RowSums{p[0], p[1], p[2]}, c);
     }
     x = join_lanes<64>(x, c);
-    if (threadIdx.x == 0) finish(a, r, x, c, at_target);
+    if (threadIdx.x == 0) finish(a, r, x, to_log2, at_target);
 }
 
 template <bool F32>
@@ -136,7 +139,7 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobGradArgs a
     const bool padding = (unsigned)target >= (unsigned)a.vocab;
     const Row row(a.logits, r, a.stride, a.vocab);
     const LogitRow<F32> out(a.d_logits, r, a.stride, a.vocab);
-    const float c = log2_scale(a.temperature, r), inverse = c * (float)kLn2;
+    const float c = (float)log2_scale(a.temperature, r), inverse = c * (float)kLn2;
     const float m = a.stats[2 * (int64_t)r], log2_sum = a.stats[2 * (int64_t)r + 1];
     const float g = padding ? 0.f : a.d_logprobs[r], h = padding || !a.d_entropy ? 0.f : a.d_entropy[r];
     const float entropy = a.d_entropy && !padding ? a.entropy[r] : 0.f, at_target = log2_sum == __builtin_inff() ? 0.f : g;
