@@ -72,6 +72,10 @@ class Rollout:
     """A batch of sequences: `uniform` [max_new][B] are the random numbers, temperature, top_k and top_p [B] the rows' limits."""
 
     def __init__(self, model, prompts, max_new, pages, stop, uniform, temperature, top_k=None, top_p=None, device="cuda:0"):
+        if not prompts or not all(len(p) for p in prompts) or max_new < 1:
+            raise ValueError("every prompt has a token at least, and one is drawn for it")
+        if uniform.shape != (max_new, len(prompts)):
+            raise ValueError("uniform is [max_new][B]")
         self.model, self.stop, self.max_new, self.device = model, stop, max_new, torch.device(device)
         self.uniform, self.temperature, self.top_k, self.top_p = uniform, temperature, top_k, top_p
         B, d = len(prompts), model.head_dim

@@ -147,3 +147,11 @@ def test_refusals(ex, monkeypatch):
     for args in ((x, y[:3], t), (x, y, t[:3]), (x[0], y, t), (x[None], y, t), (x, y[:, None], t), (x, y, t[:, None]), (torch.zeros(4, 0), y, t)):
         with pytest.raises(ValueError):
             ex.TokenLogprobs.apply(*args)
+
+
+def test_rollouts_that_cannot_begin(ex):
+    """A sequence without a token has no logits to draw from (those of the one before it would be taken), and each step of each sequence has a random number."""
+    u = torch.zeros(4, 2)
+    for prompts, max_new, uniform in (([[1, 2], []], 4, u), ([[], [3]], 4, u), ([], 4, u[:, :0]), ([[1], [2]], 0, u[:0]), ([[1], [2]], 5, u), ([[1], [2]], 4, u.t()), ([[1]], 4, u)):
+        with pytest.raises(ValueError):
+            ex.Rollout(None, prompts, max_new, 10, 0, uniform, None)
