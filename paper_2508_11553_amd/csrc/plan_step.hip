@@ -319,7 +319,8 @@ hipError_t launch_plan(const PlanArgs &a, hipStream_t stream)
 {
     // One workgroup is sooner while few pages come back, two kernels take the same whatever comes back.  us, one : two: 64 sequences 6.4 : 9.2, 3 of them finished with 900
     // pages 10.2 : 9.8, 6 with 7 k pages 22.6 : 9.9; 512 7.2 : 9.6; 1000 9.0 : 10.4, 100 of them finished with 6.5 k pages 35 : 10.5, 300 with 95 k 173 : 10.6.  In a rollout as
-    // many pages come back as are taken, one in 16 tokens, though some steps see many: few sequences, one workgroup.
+    // many pages come back as are taken, one in 16 tokens, though some steps see many, and the host does not know which: few sequences, one workgroup, which costs a step in
+    // which long ones end up to 13 us; 257 to 1024 sequences, two kernels, which cost a step in which few end 1.4 to 2.4 us.
     if (a.B <= 256 && a.max_rows <= 1024) {
         hipLaunchKernelGGL((plan_kernel<256>), dim3(1), dim3(256), 0, stream, a);
     } else {

@@ -6,13 +6,16 @@
 // All three limits keep a beginning of the order, so what is kept is known by its last logit (`bound`) and by the index of the
 // last one equal to it that stays.
 //
-// Weights are whole numbers: w 2^43, rounded, from an exponential in 64 bits (which costs this machine no more instructions' time than one in 32).  Their
-// sums are exact, so neither atomics nor the number of waves on a row change a token: what is added in floating point, the sums of stretches of
-// 2048 logits, is added in an order that the row alone fixes.
+// Weights are whole numbers: w 2^43, rounded, from an exponential in 64 bits.  Their sums are exact, so neither atomics nor the number of waves on a row
+// change a token: what is added in floating point, the sums of stretches of 2048 logits, is added in an order that the row alone fixes.  An instruction in
+// 64 bits takes no longer here than one in 32, but a weight takes 11 where 32 bits would do with about half: some 15 of the first kernel's 43 us for many rows of
+// bf16, none where memory bounds it.  Sums in 32 bits would be off by 1e-7 of a row and more, by how much depending on the waves' number: in nearly even rows, where a token of
+// 10^5 holds 1e-5, a hundredth of the draws would end at a neighbour.
 //
 // First kernel, a wave per stretch: its largest logit, its weights' sum relative to that (one pass over the logits, in registers), and the largest logit
-// of each lane's 32.  Bound by the vector units where there are many rows (512 of 160001 bf16: 43 us, 3.8 TB/s, 540 instructions a wave of which 430 make 32 weights a
-// lane; memory alone 25; two or four stretches to a wave are no faster), by memory for fp32 (200 of 100003: 15 us, 5.3 TB/s).
+// of each lane's 32.  Bound by the vector units where there are many rows (512 of 160001 bf16: 43 us, 3.8 TB/s; 540 instructions a wave, 36 us at the 4 cycles that each
+// takes at least: 358 for 32 weights a lane, 49 for its maxima, 42 for a power of the table, 55 for the wave's sum and maximum, 36 for the rest; memory alone 25; two or four
+// stretches to a wave are no faster), by memory for fp32 (200 of 100003: 15 us, 5.3 TB/s).
 //
 // Second kernel: of a row without limits the stretch in which the draw ends, by one wave each for itself, and the token in it (7 us for 512 rows: five trips to memory).
 // Of a row with limits a workgroup first looks at the lanes' maxima: the k-th largest of some of the logits, or one down to which some of them hold the
